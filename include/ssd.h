@@ -42,7 +42,7 @@
 extern "C" {
 #endif
 
-typedef enum { SSD_F32 = 0, SSD_BF16 = 1 } ssd_dtype;
+typedef enum { SSD_F32 = 0, SSD_BF16 = 1, SSD_F16 = 2 } ssd_dtype;   /* SSD_F16: caches only */
 
 /* return codes */
 enum {
@@ -62,6 +62,10 @@ enum {
     SSD_UTT_BAD_DRAFT_ID = 2u,  /* a draft id outside [0,V): treated as rejected, never read */
     SSD_UTT_BAD_OFFSETS = 4u,   /* off[b] < 0, off[b+1] < off[b] or off[b+1] > rows: utterance
                                    treated as empty and never accepted */
+    SSD_UTT_BAD_PARENT = 8u,    /* a node's parent is outside [-1, its own index) */
+    SSD_UTT_BAD_CACHE = 16u,    /* a cache length outside [0, the page table's room], or a page
+                                   outside [0, pages) among those that the length covers */
+    SSD_UTT_CACHE_FULL = 32u,   /* ssd_cache_append: no room for the path; nothing was written */
     SSD_UTT_INTERNAL = 0x80000000u /* a bounded wait inside a kernel ran out while this utterance
                                       was processed: discard every output of the call */
 };
@@ -389,6 +393,62 @@ int32_t ssd_verify_combine(const float *stats_all, int32_t R, int64_t V_total,
                            float *token_logp, float *row_lse,
                            int32_t *accepted_len, uint8_t *all_accepted, uint32_t *utt_status,
                            void *stream);
+
+/*
+ * Draft trees and the key/value cache they are verified against.
+ *
+ * A draft need not be a single sequence: hypotheses that share prefixes form a tree, and one LLM
+ * pass scores all of its nodes.  (The paper verifies the one greedy CTC hypothesis, Section 2.2; a
+ * tree of one path is that.)  The rows of utterance b in [tok_off[b], tok_off[b+1]) are its nodes.
+ * parent[i] is the index WITHIN THE UTTERANCE of the node that node i continues, smaller than i's
+ * own, or -1 for a node that continues the cached context itself; parent == NULL means a chain
+ * (node i continues node i - 1).  A node's line of descent is the node, its parent, and so on.
+ *
+ * The keys and values of the context lie in a paged cache: utterance b's slot s is slot
+ * s % page_size of page page_table[b * table_stride + s / page_size].  Nodes' own keys and values
+ * stay outside of it, in ragged arrays beside q, until ssd_cache_append writes those of the
+ * accepted path behind the context: nothing of a rejected node ever enters the cache.
+ *
+ * Keys, values, queries and attention outputs are SSD_BF16 or SSD_F16, heads are 64 or 128 values
+ * long and contiguous; every base address and every stride of an axis with more than one entry is a
+ * multiple of 16 bytes (else SSD_ERR_ALIGN).  Strides count elements.
+ */
+typedef struct ssd_heads {     /* an array [M, heads, head_dim] */
+    void *data;
+    int64_t row_stride, head_stride;
+    int32_t heads;
+} ssd_heads;
+typedef struct ssd_kv_cache {  /* k and v: [pages, page_size, heads, head_dim], strides alike */
+    void *k, *v;
+    int64_t page_stride, slot_stride, head_stride;
+    int32_t pages, page_size, heads, head_dim;
+    ssd_dtype dtype;
+    int32_t max_pages;             /* entries of a page table's row */
+    const int32_t *page_table;     /* device, [B, table_stride] */
+    int64_t table_stride;
+    const int32_t *len;            /* device, [B]: slots in use */
+} ssd_kv_cache;
+
+/*
+ * Attention of every node to its utterance's cache and to its own line of descent.
+ *   s_ij   = scale q_i . k_j,  or  cap tanh(scale q_i . k_j / cap)  where cap > 0
+ *   out_i  = sum_j softmax_j(s_ij) v_j     over the cached slots and the nodes of i's line
+ *   lse[i, head] = log sum_j exp(s_ij)                                            (nullable)
+ * q [M, Hq, D], tree_k, tree_v [M, Hkv, D], out [M, Hq, D] (same type); Hq a multiple of Hkv, at most
+ * 128 times it; query head h reads kv head h / (Hq / Hkv).  max_nodes: the most nodes that an
+ * utterance has; one that has more is left out (SSD_UTT_BAD_OFFSETS, its rows untouched), as one
+ * with malformed offsets is.  A parent out of range counts as -1 (SSD_UTT_BAD_PARENT).  A cache length out
+ * of range is clamped and a bad page reads as zeros (SSD_UTT_BAD_CACHE): nothing outside the
+ * cache is touched.  Keys and values of nodes that are not on a row's line, and what the cache
+ * holds behind len, have no influence on it, NaN and infinities included.
+ * utt_status [B] u32 (overwritten).  cache->k and ->v may be NULL with pages == 0.
+ * Errors: SSD_ERR_NULL, SSD_ERR_ARG (sizes, head counts, head_dim, a scale that is not positive and
+ * finite, a cap that is negative or not finite), SSD_ERR_DTYPE, SSD_ERR_ALIGN, SSD_ERR_CUDA.
+ */
+int32_t ssd_tree_attention(const ssd_heads *q, const ssd_heads *tree_k, const ssd_heads *tree_v,
+                           const ssd_kv_cache *cache, const int64_t *tok_off, const int32_t *parent,
+                           int32_t B, int64_t M, int32_t max_nodes, float scale, float cap,
+                           const ssd_heads *out, float *lse, uint32_t *utt_status, void *stream);
 
 /*
  * Read-span hooks.  The paper has no counterpart: these are test hooks of this library, host

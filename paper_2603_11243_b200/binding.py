@@ -19,8 +19,9 @@ import torch
 
 from . import build as _build
 
-F32, BF16 = 0, 1
+F32, BF16, F16 = 0, 1, 2
 UTT_NONFINITE, UTT_BAD_DRAFT_ID, UTT_BAD_OFFSETS, UTT_INTERNAL = 1, 2, 4, 0x80000000
+UTT_BAD_PARENT, UTT_BAD_CACHE, UTT_CACHE_FULL = 8, 16, 32
 OK, ERR_NULL, ERR_ARG, ERR_DTYPE, ERR_WORKSPACE, ERR_CUDA, ERR_ALIGN, ERR_TOO_LARGE = range(8)
 VERIFY_STATIC_SCRATCH_BYTES = 8 << 20
 
@@ -43,6 +44,19 @@ class LaunchOpts(C.Structure):
                 ("stages", C.c_int32), ("stage_bytes", C.c_int32), ("split", C.c_int32),
                 ("ev_begin", C.c_void_p), ("ev_end", C.c_void_p), ("fma_exp", C.c_int32),
                 ("finish", C.c_int32)]
+
+
+class Heads(C.Structure):
+    """Mirror of ssd_heads (include/ssd.h)."""
+    _fields_ = [("data", C.c_void_p), ("row_stride", C.c_int64), ("head_stride", C.c_int64), ("heads", C.c_int32)]
+
+
+class KvCache(C.Structure):
+    """Mirror of ssd_kv_cache (include/ssd.h)."""
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("page_stride", C.c_int64), ("slot_stride", C.c_int64),
+                ("head_stride", C.c_int64), ("pages", C.c_int32), ("page_size", C.c_int32), ("heads", C.c_int32),
+                ("head_dim", C.c_int32), ("dtype", C.c_int), ("max_pages", C.c_int32), ("page_table", C.c_void_p),
+                ("table_stride", C.c_int64), ("len", C.c_void_p)]
 
 
 _lib = None
@@ -125,6 +139,8 @@ def lib():
         L.ssd_greedy_step.restype = i32
         L.ssd_greedy_step.argtypes = [vp, C.c_int, i32, i64, i64, vp, vp, vp, vp, vp, C.c_size_t,
                                       vp, vp]
+        L.ssd_tree_attention.restype = i32
+        L.ssd_tree_attention.argtypes = [vp, vp, vp, vp, vp, vp, i32, i64, i32, C.c_float, C.c_float, vp, vp, vp, vp]
         _lib = L
     return _lib
 
@@ -587,6 +603,94 @@ def ssd_greedy_step(logits: torch.Tensor, V: Optional[int] = None, out=None,
         _opts(opts))
     if rc != OK:
         raise SsdError(rc, "ssd_greedy_step")
+    return out
+
+
+# ---- draft trees and their cache ---------------------------------------------------------------
+
+def _heads(x: torch.Tensor, name: str) -> Heads:
+    if x.dim() != 3 or (x.shape[2] > 1 and x.stride(2) != 1):
+        raise ValueError("%s must be [rows, heads, head_dim] with contiguous heads" % name)
+    return Heads(_dev(x, name), x.stride(0), x.stride(1), x.shape[1])
+
+
+def _kv_code(t: torch.Tensor) -> int:
+    if t.dtype == torch.bfloat16:
+        return BF16
+    if t.dtype == torch.float16:
+        return F16
+    raise TypeError("keys and values must be bfloat16 or float16, got %s" % t.dtype)
+
+
+def _kv_cache(k_cache: torch.Tensor, v_cache: Optional[torch.Tensor], page_table: torch.Tensor,
+              cache_len: torch.Tensor, B: int) -> KvCache:
+    if k_cache.dim() != 4 or (k_cache.shape[3] > 1 and k_cache.stride(3) != 1):
+        raise ValueError("k_cache must be [pages, page_size, heads, head_dim] with contiguous heads")
+    if v_cache is not None and (v_cache.dtype != k_cache.dtype or v_cache.shape != k_cache.shape or
+                                any(n > 1 and a != b for n, a, b in zip(k_cache.shape, v_cache.stride(), k_cache.stride()))):
+        raise ValueError("v_cache must have k_cache's type, shape and strides")
+    if page_table.dtype != torch.int32 or cache_len.dtype != torch.int32:
+        raise TypeError("page_table and cache_len must be int32")
+    if page_table.dim() != 2 or page_table.shape[0] != B or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
+        raise ValueError("page_table must be [B, max_pages] with contiguous rows")
+    if cache_len.dim() != 1 or cache_len.shape[0] != B or (B > 1 and cache_len.stride(0) != 1):
+        raise ValueError("cache_len must be a contiguous [B]")
+    pages, page, heads, D = k_cache.shape
+    return KvCache(_dev(k_cache, "k_cache"), _dev(v_cache, "v_cache"), k_cache.stride(0), k_cache.stride(1),
+                   k_cache.stride(2), pages, page, heads, D, _kv_code(k_cache), page_table.shape[1],
+                   _dev(page_table, "page_table"), max(page_table.stride(0), page_table.shape[1]) if B <= 1 else page_table.stride(0),
+                   _dev(cache_len, "cache_len"))
+
+
+def _ref(x):
+    return C.cast(C.pointer(x), C.c_void_p)
+
+
+def _nodes(tok_off: torch.Tensor, parent: Optional[torch.Tensor], M: int) -> int:
+    if tok_off.dtype != torch.int64 or tok_off.dim() != 1 or not tok_off.is_contiguous():
+        raise TypeError("tok_off must be a contiguous int64 [B + 1]")
+    if parent is not None and (parent.dtype != torch.int32 or parent.shape != (M,) or not parent.is_contiguous()):
+        raise TypeError("parent must be a contiguous int32 [M]")
+    return tok_off.shape[0] - 1
+
+
+def alloc_tree_attention_outputs(M: int, B: int, heads: int, head_dim: int, dtype, device) -> Dict[str, torch.Tensor]:
+    return dict(out=torch.empty((M, heads, head_dim), dtype=dtype, device=device),
+                lse=torch.empty((M, heads), dtype=torch.float32, device=device),
+                utt_status=torch.empty((B,), dtype=torch.int32, device=device))
+
+
+def ssd_tree_attention(q: torch.Tensor, tree_k: torch.Tensor, tree_v: torch.Tensor, k_cache: torch.Tensor,
+                       v_cache: torch.Tensor, page_table: torch.Tensor, cache_len: torch.Tensor,
+                       tok_off: torch.Tensor, max_nodes: int, parent: Optional[torch.Tensor] = None,
+                       scale: Optional[float] = None, cap: float = 0.0, out=None) -> Dict[str, torch.Tensor]:
+    """Attention of every draft node to its utterance's paged cache and to its own line of descent
+    (one layer of the pass that Section 2.2 verifies with).  q [M, Hq, D]; tree_k, tree_v [M, Hkv, D];
+    k_cache, v_cache [pages, page_size, Hkv, D]; parent None: chains; scale None: D ** -0.5; scores capped
+    at cap by a tanh where cap > 0.  Returns out [M, Hq, D], lse [M, Hq] and utt_status [B]."""
+    M, B = q.shape[0], _nodes(tok_off, parent, q.shape[0])
+    if tree_k.dtype != q.dtype or tree_v.dtype != q.dtype or k_cache.dtype != q.dtype:
+        raise TypeError("q, tree_k, tree_v and the cache must have one type")
+    for name, x in (("tree_k", tree_k), ("tree_v", tree_v)):
+        if x.dim() != 3 or x.shape[0] != M or x.shape[2] != q.shape[2]:
+            raise ValueError("%s must be [M, heads, head_dim] like q" % name)
+    if k_cache.dim() != 4 or k_cache.shape[3] != q.shape[2]:
+        raise ValueError("the cache's heads are not as long as q's")
+    if out is None:
+        out = alloc_tree_attention_outputs(M, B, q.shape[1], q.shape[2], q.dtype, q.device)
+    o, lse = out["out"], out.get("lse")
+    if o.dtype != q.dtype or o.shape != q.shape:
+        raise ValueError("out must have q's type and shape")
+    if lse is not None and (lse.dtype != torch.float32 or lse.shape != q.shape[:2] or not lse.is_contiguous()):
+        raise ValueError("lse must be a contiguous float32 [M, heads]")
+    cache = _kv_cache(k_cache, v_cache, page_table, cache_len, B)
+    rc = lib().ssd_tree_attention(
+        _ref(_heads(q, "q")), _ref(_heads(tree_k, "tree_k")), _ref(_heads(tree_v, "tree_v")), _ref(cache),
+        _dev(tok_off, "tok_off"), _dev(parent, "parent"), B, M, max_nodes,
+        q.shape[2] ** -0.5 if scale is None else scale, cap, _ref(_heads(o, "out")), _dev(lse, "lse"),
+        _dev(out["utt_status"], "utt_status"), _stream())
+    if rc != OK:
+        raise SsdError(rc, "ssd_tree_attention")
     return out
 
 

@@ -1,5 +1,7 @@
 // The C ABI of libssd: argument validation and dispatch.  Every step of the path runs in the
 // kernels of ssd_ctc.cu and ssd_verify.cu; nothing here computes.
+#include <math.h>
+
 #include <atomic>
 #include <map>
 #include <mutex>
@@ -346,6 +348,53 @@ int32_t ssd_greedy_step(const void *logits, ssd_dtype dtype, int32_t V, int64_t 
     Launch L{static_cast<cudaStream_t>(stream), opts};
     return launch_greedy(logits, dtype, V, ld, R, workspace, next_token, next_logp, row_lse,
                          row_status, plan, L);
+}
+
+// What the calls on a cache ask of it.  `values`: whether they touch its values as well as its keys.
+static int check_cache(const ssd_kv_cache &c, int32_t B, bool values) {
+    if (c.dtype != SSD_BF16 && c.dtype != SSD_F16) return SSD_ERR_DTYPE;
+    if (c.pages < 0 || c.page_size < 1 || c.heads < 1 || c.max_pages < 0 || (c.head_dim != 64 && c.head_dim != 128))
+        return SSD_ERR_ARG;
+    if (c.table_stride < (B > 1 ? c.max_pages : 0)) return SSD_ERR_ARG;
+    if (B > 0 && (!c.len || (c.max_pages > 0 && !c.page_table))) return SSD_ERR_NULL;
+    if (c.pages > 0 && (!c.k || (values && !c.v))) return SSD_ERR_NULL;
+    if (c.page_stride < 0 || c.slot_stride < 0 || c.head_stride < 0) return SSD_ERR_ARG;
+    if (reinterpret_cast<uintptr_t>(c.k) % 16 || (values && reinterpret_cast<uintptr_t>(c.v) % 16)) return SSD_ERR_ALIGN;
+    if ((c.heads > 1 && c.head_stride % 8) || (c.page_size > 1 && c.slot_stride % 8) || (c.pages > 1 && c.page_stride % 8))
+        return SSD_ERR_ALIGN;
+    // a tensor map holds strides below 2^40 bytes
+    const int64_t most = (1ll << 39) - 8;
+    if ((c.heads > 1 && c.head_stride > most) || (c.page_size > 1 && c.slot_stride > most) || (c.pages > 1 && c.page_stride > most))
+        return SSD_ERR_ARG;
+    return SSD_OK;
+}
+static int check_heads(const ssd_heads &x, int64_t M) {
+    if (x.heads < 1 || x.row_stride < 0 || x.head_stride < 0) return SSD_ERR_ARG;
+    if (M > 0 && !x.data) return SSD_ERR_NULL;
+    if (reinterpret_cast<uintptr_t>(x.data) % 16 || (x.heads > 1 && x.head_stride % 8) || (M > 1 && x.row_stride % 8))
+        return SSD_ERR_ALIGN;
+    const int64_t most = (1ll << 39) - 8;
+    if ((x.heads > 1 && x.head_stride > most) || (M > 1 && x.row_stride > most)) return SSD_ERR_ARG;
+    return SSD_OK;
+}
+static bool check_scores(float scale, float cap) { return scale > 0.f && scale < INFINITY && cap >= 0.f && cap < INFINITY; }
+
+int32_t ssd_tree_attention(const ssd_heads *q, const ssd_heads *tree_k, const ssd_heads *tree_v,
+                           const ssd_kv_cache *cache, const int64_t *tok_off, const int32_t *parent,
+                           int32_t B, int64_t M, int32_t max_nodes, float scale, float cap,
+                           const ssd_heads *out, float *lse, uint32_t *utt_status, void *stream) {
+    if (!q || !tree_k || !tree_v || !cache || !out || !tok_off) return SSD_ERR_NULL;
+    if (B < 0 || M < 0 || M > INT32_MAX || max_nodes < 0 || !check_scores(scale, cap)) return SSD_ERR_ARG;
+    int rc = check_cache(*cache, B, true);
+    for (const ssd_heads *x : {q, tree_k, tree_v, out})
+        if (rc == SSD_OK) rc = check_heads(*x, M);
+    if (rc != SSD_OK) return rc;
+    if (q->heads % cache->heads || q->heads / cache->heads > 128 || tree_k->heads != cache->heads ||
+        tree_v->heads != cache->heads || out->heads != q->heads)
+        return SSD_ERR_ARG;
+    if (B > 0 && !utt_status) return SSD_ERR_NULL;
+    return launch_tree_attention(*q, *tree_k, *tree_v, *cache, tok_off, parent, B, M, max_nodes, scale, cap, *out, lse,
+                                 utt_status, static_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

@@ -596,4 +596,9 @@ struct PlanReplay {
 // if a launch needs more than any before it).
 cudaError_t ensure_dynamic_smem(const void *kernel, size_t bytes);
 
+// ---- draft trees and their cache (ssd_tree.cu, ssd_cache.cu) -------------------------------------
+int launch_tree_attention(const ssd_heads &q, const ssd_heads &tree_k, const ssd_heads &tree_v, const ssd_kv_cache &cache,
+                          const int64_t *tok_off, const int32_t *parent, int B, int64_t M, int max_nodes, float scale,
+                          float cap, const ssd_heads &out, float *lse, uint32_t *status, cudaStream_t stream);
+
 }  // namespace ssd

@@ -1,0 +1,212 @@
+// Wrappers of the sm_100a instructions that the cache's kernels are built from: tensor-map copies,
+// 5th-generation tensor-core products with their accumulators in tensor memory, and the layouts
+// both agree on.
+//
+// Layout of every operand tile in shared memory: rows of 64 sixteen-bit values (128 bytes), the
+// 16-byte units of a row XORed with the row's number modulo 8 (the 128-byte swizzle), 1,024-byte
+// aligned.  A head of D values is D / 64 such blocks one behind the other, each of 128 rows.  Read
+// along a row it is a K-major operand (queries and keys in the scores); read along the rows it is
+// the MN-major one (values in the second product).
+#pragma once
+
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "ssd_common.cuh"
+
+namespace ssd {
+namespace tc {
+
+constexpr int kTile = 128;                       // rows of a tile: queries, and keys
+constexpr int kBlockBytes = kTile * 128;         // 64 columns of a tile
+
+// ---- tensor-map copies -------------------------------------------------------------------------
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+        ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z)
+        : "memory");
+}
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap *map, int x, int y, int z, int w, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+        ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(w)
+        : "memory");
+}
+__device__ __forceinline__ void tma_prefetch_map(const CUtensorMap *map) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
+}
+
+// ---- tensor memory -------------------------------------------------------------------------------
+// Taken before griddepcontrol.launch_dependents: once a successor may start, everyone of this grid
+// already has its columns, so neither waits for the other's.
+__device__ __forceinline__ void tmem_alloc(uint32_t dst_smem, uint32_t columns) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(dst_smem), "r"(columns) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_free(uint32_t addr, uint32_t columns) {
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(columns) : "memory");
+}
+__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// 32 columns of the warp's 32 lanes: lane i of the warp gets row i.
+__device__ __forceinline__ void tmem_ld32(uint32_t addr, float *r) {
+    uint32_t *u = reinterpret_cast<uint32_t *>(r);
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]),
+          "=r"(u[8]), "=r"(u[9]), "=r"(u[10]), "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15]),
+          "=r"(u[16]), "=r"(u[17]), "=r"(u[18]), "=r"(u[19]), "=r"(u[20]), "=r"(u[21]), "=r"(u[22]), "=r"(u[23]),
+          "=r"(u[24]), "=r"(u[25]), "=r"(u[26]), "=r"(u[27]), "=r"(u[28]), "=r"(u[29]), "=r"(u[30]), "=r"(u[31])
+        : "r"(addr));
+}
+__device__ __forceinline__ void tmem_st32(uint32_t addr, const float *r) {
+    const uint32_t *u = reinterpret_cast<const uint32_t *>(r);
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
+        ::"r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]),
+          "r"(u[8]), "r"(u[9]), "r"(u[10]), "r"(u[11]), "r"(u[12]), "r"(u[13]), "r"(u[14]), "r"(u[15]),
+          "r"(u[16]), "r"(u[17]), "r"(u[18]), "r"(u[19]), "r"(u[20]), "r"(u[21]), "r"(u[22]), "r"(u[23]),
+          "r"(u[24]), "r"(u[25]), "r"(u[26]), "r"(u[27]), "r"(u[28]), "r"(u[29]), "r"(u[30]), "r"(u[31]), "r"(addr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t *u) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
+        ::"r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]),
+          "r"(u[8]), "r"(u[9]), "r"(u[10]), "r"(u[11]), "r"(u[12]), "r"(u[13]), "r"(u[14]), "r"(u[15]), "r"(addr)
+        : "memory");
+}
+
+// ---- products --------------------------------------------------------------------------------------
+// Shared-memory descriptor of an operand at `addr`, 128-byte swizzle: bits 0-13 address / 16,
+// 16-29 leading offset / 16, 32-45 stride offset / 16, 46-47 the descriptor's version, 61-63 swizzle.
+// K-major: 8 rows lie 1,024 bytes apart (the leading offset is not looked at).  MN-major: 8 rows of
+// the K axis lie 1,024 bytes apart, blocks of 64 columns kBlockBytes.
+__device__ __forceinline__ uint64_t operand(uint32_t addr) {
+    return (uint64_t)((addr & 0x3ffff) >> 4) | (uint64_t)(kBlockBytes >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 |
+           (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+// Instruction descriptor: fp32 accumulators, both operands of one 16-bit type, M = 128.
+template <typename T> struct Format;
+template <> struct Format<__half> { static constexpr uint32_t kCode = 0, kExponent = 0x7c00; };
+template <> struct Format<__nv_bfloat16> { static constexpr uint32_t kCode = 1, kExponent = 0x7f80; };
+template <typename T> __device__ __forceinline__ uint32_t instruction(uint32_t n, bool b_mn_major) {
+    return 1u << 4 | Format<T>::kCode << 7 | Format<T>::kCode << 10 | (b_mn_major ? 1u << 16 : 0u) | (n >> 3) << 17 |
+           (uint32_t)(kTile >> 4) << 24;
+}
+// d (+)= a . b; a and b in shared memory
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)accumulate)
+        : "memory");
+}
+// d (+)= a . b; a in tensor memory
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+        ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)accumulate)
+        : "memory");
+}
+// arrives on `bar` once every product this thread has issued so far is complete
+__device__ __forceinline__ void mma_commit(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+
+// ---- small arithmetic -----------------------------------------------------------------------------
+template <typename T> __device__ __forceinline__ uint32_t pack2(float lo, float hi);
+template <> __device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+template <> __device__ __forceinline__ uint32_t pack2<__half>(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+// where the 16-byte unit `unit` of row `row` of a tile lies
+__device__ __forceinline__ uint32_t unit_at(uint32_t tile, int row, int unit) {
+    return tile + (unit >> 3) * kBlockBytes + row * 128 + (((unit & 7) ^ (row & 7)) << 4);
+}
+__device__ __forceinline__ void named_sync(int id, int threads) {
+    asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
+}
+__device__ __forceinline__ float4 cluster_ld4(uint32_t a) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ float2 cluster_ld2(uint32_t a) {
+    float2 v;
+    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(a) : "memory");
+    return v;
+}
+
+// ---- the paged cache's tiles ------------------------------------------------------------------------
+// A tile is up to 128 consecutive slots that end within `pages` whole pages (pages of up to 64 slots,
+// a multiple of 8: as many as fit; other pages of up to 128: one) or within one page (larger pages).
+struct Paging {
+    int page;          // slots of a page
+    int pages;         // pages of a tile; 0: tiles within a page
+    int per_page;      // tiles of a page where pages == 0
+    int box;           // slots that one copy brings
+};
+inline Paging paging(int page) {
+    Paging p{};
+    p.page = page;
+    if (page <= kTile) {
+        p.pages = page <= 64 && page % 8 == 0 ? kTile / page : 1;
+        p.box = page;
+    } else {
+        p.per_page = (page + kTile - 1) / kTile;
+        p.box = 64;
+    }
+    return p;
+}
+struct TileAt {
+    int page, slot, valid;    // first page (of the utterance's table), first slot in it, slots that count
+};
+__host__ __device__ inline int paged_tiles(const Paging &p, int len) {
+    if (p.pages) return (len + p.pages * p.page - 1) / (p.pages * p.page);
+    const int whole = len / p.page, rest = len - whole * p.page;
+    return whole * p.per_page + (rest + kTile - 1) / kTile;
+}
+__host__ __device__ inline TileAt paged_tile(const Paging &p, int len, int t) {
+    TileAt a;
+    if (p.pages) {
+        a.page = t * p.pages;
+        a.slot = 0;
+        const int left = len - a.page * p.page, most = p.pages * p.page;
+        a.valid = left < most ? left : most;
+    } else {
+        a.page = t / p.per_page;
+        a.slot = (t - a.page * p.per_page) * kTile;
+        const int in_page = p.page - a.slot, left = len - a.page * p.page - a.slot;
+        a.valid = in_page < kTile ? in_page : kTile;
+        if (left < a.valid) a.valid = left;
+    }
+    return a;
+}
+
+}  // namespace tc
+
+// ---- host: tensor maps ---------------------------------------------------------------------------
+// dims[0] is the innermost axis (contiguous); strides[i] is axis i + 1's, in bytes.  False: the
+// driver refused (or there is none); record_cuda_error has been called.
+bool encode_map(CUtensorMap *map, ssd_dtype dtype, const void *base, int rank, const uint64_t *dims,
+                const uint64_t *strides, const uint32_t *box);
+
+}  // namespace ssd

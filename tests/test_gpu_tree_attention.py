@@ -1,0 +1,207 @@
+"""ssd_tree_attention against the definition in 64 bits.
+
+Tolerances.  Scores are sums of D exact products of two 16-bit values in fp32 and one fp32 scaling; with
+|q.k| terms of a few units their absolute error stays below 1e-5, which is the relative error of every
+probability and the absolute error of the log-sum-exp (held to 2e-5 plus 2^-23 of its size).  An output is
+a mean of values v with weights p: each p is rounded once to the 16-bit type (relative half step u = 2^-8 or
+2^-11, so the error is at most u * sum p |v|), and so is the result (u * |out|): the bound is
+u * (mean |v| + |out|) with a tenth more for the rest."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2603_11243_b200 import binding as ssd
+from tree_ref import Case
+
+pytestmark = pytest.mark.gpu
+HALF_STEP = {torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
+
+
+def run(c, dev, cap=0.0, d=None, **kw):
+    d = d or c.on(dev)
+    r = ssd.ssd_tree_attention(d["q"], d["tk"], d["tv"], d["k"], d["v"], d["table"], d["lens"], d["off"], c.max_nodes,
+                               d["parent"], c.scale, cap, **kw)
+    torch.cuda.synchronize()
+    return r
+
+
+def check(c, r, cap=0.0, rows=None):
+    out, lse = c.attention(cap)
+    keep = c.v, c.tv
+    c.v, c.tv = c.v.abs(), c.tv.abs()
+    mean, _ = c.attention(cap)
+    c.v, c.tv = keep
+    u = HALF_STEP[c.dtype]
+    rows = slice(None) if rows is None else rows
+    got, want = r["out"].cpu().double()[rows], out[rows]
+    bound = 1.1 * u * (mean[rows] + want.abs()) + 1e-6
+    worst = ((got - want).abs() / bound).max().item() if got.numel() else 0.0
+    assert worst <= 1.0, worst
+    dl = (r["lse"].cpu().double()[rows] - lse[rows]).abs()
+    assert (dl <= 2e-5 + 2.0 ** -23 * lse[rows].abs()).all(), dl.max()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n,lens", [([1], [1]), ([1], [0]), ([1], [1000]), ([5], [128]), ([7, 0, 3], [130, 50, 0]),
+                                    ([20, 31, 17], [700, 127, 257])])
+def test_against_64_bits(cuda_device, dtype, D, n, lens):
+    c = Case(1, n, lens, D=D, dtype=dtype).spoil_unused()
+    r = run(c, cuda_device)
+    check(c, r)
+    assert (r["utt_status"] == 0).all()
+
+
+@pytest.mark.parametrize("Hq,Hkv", [(1, 1), (4, 4), (5, 1), (28, 4), (6, 2), (16, 1), (128, 1)])
+def test_head_layouts(cuda_device, Hq, Hkv):
+    c = Case(2, [9, 3, 40], [200, 33, 300], Hq=Hq, Hkv=Hkv).spoil_unused()
+    check(c, run(c, cuda_device))
+
+
+@pytest.mark.parametrize("page", [1, 3, 8, 20, 24, 64, 100, 128, 129, 200, 256, 1000])
+def test_pages_that_end_inside_a_tile(cuda_device, page):
+    c = Case(3, [4, 9, 2], [301, 127, 129], page=page).spoil_unused()
+    check(c, run(c, cuda_device))
+
+
+@pytest.mark.parametrize("chain", [True, False])
+@pytest.mark.parametrize("n", [[33], [64, 65], [130, 1, 257], [300]])
+def test_more_nodes_than_a_tile(cuda_device, n, chain):
+    """G = 4: 32 nodes a tile, and two tiles to a CTA; over 128 nodes the tree's keys are several tiles, over 256
+    its parents are not all in shared memory."""
+    c = Case(4, n, [90] * len(n), chain=chain, roots=2 if not chain else 1, dtype=torch.float16, D=128).spoil_unused()
+    check(c, run(c, cuda_device))
+
+
+def test_many_items_leave_no_cluster(cuda_device):
+    """More items than multiprocessors: one CTA for each, both with one tile of queries and with two."""
+    rng = np.random.default_rng(5)
+    c = Case(5, rng.integers(0, 24, 41), rng.integers(0, 400, 41), Hq=16, Hkv=8).spoil_unused()
+    check(c, run(c, cuda_device))
+    c = Case(6, rng.integers(0, 150, 11), rng.integers(0, 400, 11), Hq=16, Hkv=8, chain=True, D=128).spoil_unused()
+    check(c, run(c, cuda_device))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_capped_scores(cuda_device, dtype):
+    for spread in (2.0, 30.0):
+        c = Case(7, [9, 70], [400, 90], dtype=dtype, spread=spread).spoil_unused()
+        check(c, run(c, cuda_device, cap=20.0), cap=20.0)
+
+
+def test_long_flat_tail_in_fp16(cuda_device):
+    """One score far above thousands of equal small ones, whose probabilities fp16 could not hold as they are."""
+    c = Case(8, [3], [6000], dtype=torch.float16, Hq=2, Hkv=1)
+    c.q.fill_(1.0)
+    c.k.normal_(0.0, 0.01)
+    c.tk.zero_()
+    c.k[c.table[0, 0], 0] = 2.2                                  # score 17.6: the others' p is 2e-8 each
+    check(c, run(c, cuda_device))
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("n,lens", [([6, 5], [20, 0]), ([140, 5], [20, 300]), ([6], [3000])])
+def test_what_a_node_does_not_see_cannot_reach_it(cuda_device, bad, n, lens):
+    c = Case(9, n, lens).spoil_unused()
+    d = c.on(cuda_device)
+    clean = run(c, cuda_device, d=d)
+    j = 3                                                        # a node of utterance 0, and who descends from it
+    below = [i for i in range(n[0]) if any(j == a for a in __import__("tree_ref").lines(c.parent[:n[0]])[i])]
+    others = [i for i in range(c.M) if i not in below]
+    for name in ("tk", "tv"):
+        e = dict(d, **{name: d[name].clone()})
+        e[name][j, :, 5] = bad
+        r = run(c, cuda_device, d=e)
+        assert torch.equal(r["out"][others], clean["out"][others])
+        assert torch.equal(r["lse"][others], clean["lse"][others])
+        if name == "tv":
+            hit = r["out"][below][..., 5].float()
+            assert (torch.isnan(hit) if bad != bad else torch.isinf(hit)).all()
+            assert torch.isfinite(r["out"][below][..., :5].float()).all()
+
+
+def test_strided_and_partial_inputs(cuda_device):
+    """q, keys and values as slices of one fused projection, K and V caches interleaved, out inside a wider array."""
+    c = Case(10, [9, 33], [100, 257], Hq=8, Hkv=2, D=64)
+    d = c.on(cuda_device)
+    fused = torch.randn(c.M, 8 + 2 + 2, 64, device=cuda_device).to(c.dtype)
+    fused[:, :8], fused[:, 8:10], fused[:, 10:] = d["q"], d["tk"], d["tv"]
+    d.update(q=fused[:, :8], tk=fused[:, 8:10], tv=fused[:, 10:])
+    both = torch.empty(c.k.shape[0], 2, *c.k.shape[1:], dtype=c.dtype, device=cuda_device)
+    both[:, 0], both[:, 1] = d["k"], d["v"]
+    d.update(k=both[:, 0], v=both[:, 1])
+    wide = torch.full((c.M, 10, 72), 7.0, dtype=c.dtype, device=cuda_device)
+    out = dict(out=wide[:, 1:9, :64], lse=torch.empty(c.M, 8, device=cuda_device),
+               utt_status=torch.empty(2, dtype=torch.int32, device=cuda_device))
+    r = run(c, cuda_device, d=d, out=out)
+    check(c, r)
+    assert (wide[:, 0] == 7).all() and (wide[:, 9] == 7).all() and (wide[:, :, 64:] == 7).all()
+
+
+def test_head_major_cache(cuda_device):
+    c = Case(11, [3, 4], [40, 70])
+    d = c.on(cuda_device)
+    for k in ("k", "v"):
+        d[k] = d[k].permute(0, 2, 1, 3).contiguous().permute(0, 2, 1, 3)          # [pages, heads, slots, D] in memory
+    check(c, run(c, cuda_device, d=d))
+
+
+def test_malformed_utterances(cuda_device):
+    c = Case(12, [4, 5, 6, 7], [50, 60, 70, 80])
+    d = c.on(cuda_device)
+    clean = run(c, cuda_device, d=d)
+    # a parent out of range counts as none; a bad page and a bad length are reported and stay inside the cache
+    e = dict(d, parent=d["parent"].clone(), table=d["table"].clone(), lens=d["lens"].clone())
+    e["parent"][c.off[1] + 2] = 2
+    e["parent"][c.off[1] + 3] = -5
+    e["table"][2, 1] = c.k.shape[0]
+    e["lens"][3] = c.table.shape[1] * c.page + 1
+    r = run(c, cuda_device, d=e)
+    assert r["utt_status"].cpu().tolist() == [0, ssd.UTT_BAD_PARENT, ssd.UTT_BAD_CACHE, ssd.UTT_BAD_CACHE]
+    assert torch.equal(r["out"][:4], clean["out"][:4])
+    c.parent[c.off[1] + 2] = c.parent[c.off[1] + 3] = -1
+    check(c, dict(out=r["out"], lse=r["lse"]), rows=slice(0, 9))
+    # offsets that run backwards, and more nodes than were announced: rows are left as they were
+    off = torch.tensor([0, 4, 2, 15, 22], dtype=torch.int64, device=cuda_device)
+    out = ssd.alloc_tree_attention_outputs(c.M, c.B, c.Hq, c.D, c.dtype, cuda_device)
+    out["out"].fill_(3.0)
+    r = ssd.ssd_tree_attention(d["q"], d["tk"], d["tv"], d["k"], d["v"], d["table"], d["lens"], off, 7, d["parent"], out=out)
+    assert r["utt_status"].cpu().tolist() == [0, ssd.UTT_BAD_OFFSETS, ssd.UTT_BAD_OFFSETS, 0]
+    assert (r["out"][4:15] == 3.0).all() and torch.equal(r["out"][:4], clean["out"][:4])
+
+
+def test_without_a_cache(cuda_device):
+    c = Case(13, [9, 4], [0, 0], D=128)
+    d = c.on(cuda_device)
+    d.update(k=d["k"][:0], v=d["v"][:0], table=d["table"][:, :0])
+    check(c, run(c, cuda_device, d=d))
+    none = ssd.ssd_tree_attention(d["q"][:0], d["tk"][:0], d["tv"][:0], d["k"], d["v"], d["table"][:0], d["lens"][:0],
+                                  d["off"][:1], 0, None)
+    assert none["out"].shape == (0, c.Hq, c.D)
+
+
+def test_captured_and_on_two_streams(cuda_device):
+    c = Case(14, [9, 70, 3], [500, 90, 1200])
+    other = Case(15, [30, 2, 50], [100, 1000, 20])
+    d, e = c.on(cuda_device), other.on(cuda_device)
+    want, want2 = run(c, cuda_device, d=d), run(other, cuda_device, d=e)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(10):
+        got = []
+        for s, x, y in zip(streams, (c, other), (d, e)):
+            with torch.cuda.stream(s):
+                got.append(ssd.ssd_tree_attention(y["q"], y["tk"], y["tv"], y["k"], y["v"], y["table"], y["lens"], y["off"],
+                                                  x.max_nodes, y["parent"]))
+        torch.cuda.synchronize()
+        assert torch.equal(got[0]["out"], want["out"]) and torch.equal(got[1]["out"], want2["out"])
+    out = ssd.alloc_tree_attention_outputs(c.M, c.B, c.Hq, c.D, c.dtype, cuda_device)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ssd.ssd_tree_attention(d["q"], d["tk"], d["tv"], d["k"], d["v"], d["table"], d["lens"], d["off"], c.max_nodes,
+                               d["parent"], out=out)
+    out["out"].zero_()
+    d["lens"][0] = 77                                              # a replay takes what is in the buffers then
+    graph.replay()
+    torch.cuda.synchronize()
+    c.lens[0] = 77
+    check(c, out)
