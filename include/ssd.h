@@ -451,6 +451,86 @@ int32_t ssd_tree_attention(const ssd_heads *q, const ssd_heads *tree_k, const ss
                            const ssd_heads *out, float *lse, uint32_t *utt_status, void *stream);
 
 /*
+ * Verification of a draft tree: Eq. 5 along every path at once.  logits row i is the LLM's output
+ * AFTER node i (given the context and i's line of descent), so node i is judged by its parent's row:
+ *   row_lse[i]    = log sum_v exp(x_iv)                                        (nullable)
+ *   token_logp[i] = x[parent(i), draft_ids[i]] - row_lse[parent(i)]; 0 for a node without parent
+ * A node without parent is given (the last token that is certain, whose logits the pass needs;
+ * its draft id is not looked at).  Node i is accepted iff it is given, or its parent is accepted
+ * and token_logp[i] > log(tau_slm) (ssd_verify's rule).  The result is the longest accepted path, that
+ * of the lowest last node where several are equally long (a draft lists its likelier hypotheses first):
+ *   path_len[b]               its nodes, given ones included; 0 if nothing is accepted
+ *   path[tok_off[b] + k]      k < path_len[b]: its k-th node's index within the utterance; -1 behind it
+ *   on_path[tok_off[b] + i]   1 / 0: whether node i is on it
+ * Auto-regressive decoding resumes from the logits of the path's last node.  A parent out of range
+ * makes its node rejected (SSD_UTT_BAD_PARENT).  skip [B] u8 (nullable): nonzero = not verified: the
+ * rows are not read, path_len = 0, token_logp and row_lse untouched.  Malformed offsets: path_len = 0.
+ * logits [M, ld] dtype, read once; draft_ids, parent, path [M] i32; token_logp, row_lse [M] f32;
+ * on_path [M] u8; path_len [B] i32; utt_status [B] u32.
+ * workspace: as ssd_verify (ssd_verify_workspace_bytes(B, M, V, dtype, opts)).
+ * Errors: as ssd_verify; SSD_ERR_ARG also for opts->finish == 2.
+ */
+int32_t ssd_verify_tree(const void *logits, ssd_dtype dtype, int32_t V, int64_t ld,
+                        const int64_t *tok_off, const int32_t *draft_ids, const int32_t *parent,
+                        int32_t B, int64_t M, float tau_slm, const uint8_t *skip,
+                        float *token_logp, float *row_lse, int32_t *path, int32_t *path_len,
+                        uint8_t *on_path, uint32_t *utt_status,
+                        void *workspace, size_t workspace_bytes, void *stream,
+                        const ssd_launch_opts *opts);
+
+/*
+ * The accepted path's keys and values enter the cache.  For every utterance, node path[tok_off[b] + k]
+ * (path == NULL: node k), k < path_len[b], is written to slot len[b] + k:
+ *   new_len[b] = len[b] + path_len[b]       (its own array, not cache->len)
+ *   weight[b * weight_stride + slot] = 0    for the new slots below weight_cols      (weight nullable)
+ * tree_k, tree_v as in ssd_tree_attention; path [M] i32 and path_len [B] i32 as ssd_verify_tree leaves them.
+ * Nothing is written and new_len[b] = len[b] where the pages have no room (SSD_UTT_CACHE_FULL), where
+ * offsets or len are malformed, and where path_len[b] is negative or more than the utterance's nodes
+ * (SSD_UTT_BAD_PARENT).  A path entry that is none of its nodes (SSD_UTT_BAD_PARENT) and a page outside the cache
+ * (SSD_UTT_BAD_CACHE) are left out.  Utterances may share pages, as long as no two write the same slot.
+ * Errors: SSD_ERR_NULL, SSD_ERR_ARG, SSD_ERR_DTYPE, SSD_ERR_ALIGN, SSD_ERR_CUDA.
+ */
+int32_t ssd_cache_append(const ssd_heads *tree_k, const ssd_heads *tree_v, const ssd_kv_cache *cache,
+                         const int64_t *tok_off, const int32_t *path, const int32_t *path_len,
+                         int32_t B, int64_t M, float *weight, int64_t weight_stride, int32_t weight_cols,
+                         int32_t *new_len, uint32_t *utt_status, void *stream);
+
+/*
+ * Attention weight that every cached slot has received, accumulated:
+ *   weight[b * weight_stride + s] += sum over the nodes i of b with use[i] != 0 (NULL: all) and over
+ *                                    their heads of exp(s_is - lse[i, head]),       s < len[b]
+ * with the scores of ssd_tree_attention, whose lse this takes (use: its on_path counts accepted nodes
+ * only).  Sums are fp32 and in a fixed order: the same inputs give the same bits.  Queries and lse of
+ * nodes that do not count have no influence, NaN included.  cache->v is not looked at.
+ * Slots from weight_cols on are left out (SSD_UTT_BAD_CACHE where len says there are some).
+ * Errors: as ssd_tree_attention.
+ */
+int32_t ssd_cache_weights(const ssd_heads *q, const float *lse, const ssd_kv_cache *cache,
+                          const int64_t *tok_off, int32_t B, int64_t M, int32_t max_nodes,
+                          float scale, float cap, const uint8_t *use,
+                          float *weight, int64_t weight_stride, int32_t weight_cols,
+                          uint32_t *utt_status, void *stream);
+
+/*
+ * Eviction.  A cache of more than `budget` slots keeps its first `sink`, its last `recent`, and of those
+ * between the budget - sink - recent with the largest weights (ties to the lowest slot; NaN is less
+ * than every number); a shorter cache keeps every slot.  The kept slots move down in place, in order:
+ *   kept[b * budget + j]   the slot that is now slot j; -1 behind new_len[b]
+ *   new_len[b]             min(len[b], budget)
+ *   weight_out[b * weight_out_stride + j] = weight[b * weight_stride + kept]; 0 behind      (nullable)
+ * What lies behind new_len in the cache is left as it was.  weight is not changed (weight_out is another
+ * array); new_len may be cache->len.  Pages are one utterance's own: one that two share would be
+ * compacted twice.  A len out of range is clamped, one above weight_cols (and the budget) to that; entries in
+ * bad pages are not moved (SSD_UTT_BAD_CACHE for all three).
+ * kept [B, budget] i32.
+ * Errors: SSD_ERR_NULL, SSD_ERR_ARG (also sink + recent > budget), SSD_ERR_DTYPE, SSD_ERR_ALIGN, SSD_ERR_CUDA.
+ */
+int32_t ssd_cache_evict(const ssd_kv_cache *cache, const float *weight, int64_t weight_stride,
+                        int32_t weight_cols, int32_t B, int32_t budget, int32_t sink, int32_t recent,
+                        int32_t *kept, float *weight_out, int64_t weight_out_stride,
+                        int32_t *new_len, uint32_t *utt_status, void *stream);
+
+/*
  * Read-span hooks.  The paper has no counterpart: these are test hooks of this library, host
  * only (no GPU, no stream; base_addr is an integer that is never dereferenced).
  *

@@ -141,6 +141,15 @@ def lib():
                                       vp, vp]
         L.ssd_tree_attention.restype = i32
         L.ssd_tree_attention.argtypes = [vp, vp, vp, vp, vp, vp, i32, i64, i32, C.c_float, C.c_float, vp, vp, vp, vp]
+        L.ssd_verify_tree.restype = i32
+        L.ssd_verify_tree.argtypes = [vp, C.c_int, i32, i64, vp, vp, vp, i32, i64, C.c_float, vp,
+                                      vp, vp, vp, vp, vp, vp, vp, C.c_size_t, vp, vp]
+        L.ssd_cache_append.restype = i32
+        L.ssd_cache_append.argtypes = [vp, vp, vp, vp, vp, vp, i32, i64, vp, i64, i32, vp, vp, vp]
+        L.ssd_cache_weights.restype = i32
+        L.ssd_cache_weights.argtypes = [vp, vp, vp, vp, i32, i64, i32, C.c_float, C.c_float, vp, vp, i64, i32, vp, vp]
+        L.ssd_cache_evict.restype = i32
+        L.ssd_cache_evict.argtypes = [vp, vp, i64, i32, i32, i32, i32, i32, vp, vp, i64, vp, vp, vp]
         _lib = L
     return _lib
 
@@ -691,6 +700,138 @@ def ssd_tree_attention(q: torch.Tensor, tree_k: torch.Tensor, tree_v: torch.Tens
         _dev(out["utt_status"], "utt_status"), _stream())
     if rc != OK:
         raise SsdError(rc, "ssd_tree_attention")
+    return out
+
+
+def alloc_verify_tree_outputs(M: int, B: int, device, workspace_bytes: int) -> Dict[str, torch.Tensor]:
+    e = lambda n, dt: torch.empty((n,), dtype=dt, device=device)
+    return dict(token_logp=e(M, torch.float32), row_lse=e(M, torch.float32), path=e(M, torch.int32),
+                path_len=e(B, torch.int32), on_path=e(M, torch.uint8), utt_status=e(B, torch.int32),
+                workspace=e(max(workspace_bytes, 256), torch.uint8))
+
+
+def ssd_verify_tree(logits: torch.Tensor, tok_off: torch.Tensor, draft_ids: torch.Tensor,
+                    parent: Optional[torch.Tensor], tau_slm: float, skip: Optional[torch.Tensor] = None,
+                    V: Optional[int] = None, out=None, opts: Optional[LaunchOpts] = None) -> Dict[str, torch.Tensor]:
+    """Stage 2 along a draft tree (Eq. 5 on every path): logits row i is the LLM's output after node i;
+    returns the nodes' log-likelihoods and the longest accepted path.  parent None: chains."""
+    M, ld = _rows_ld(logits)
+    V = logits.shape[1] if V is None else V
+    B = _nodes(tok_off, parent, M)
+    if draft_ids.dtype != torch.int32:
+        raise TypeError("draft_ids must be int32")
+    if skip is not None and skip.dtype != torch.uint8:
+        raise TypeError("skip must be uint8")
+    code = _dtype_code(logits)
+    if out is None:
+        out = alloc_verify_tree_outputs(M, B, logits.device, ssd_verify_workspace_bytes(B, M, V, code, opts))
+    ws = out["workspace"]
+    rc = lib().ssd_verify_tree(
+        _dev(logits, "logits"), code, V, ld, _dev(tok_off, "tok_off"), _dev(draft_ids, "draft_ids"),
+        _dev(parent, "parent"), B, M, C.c_float(tau_slm), _dev(skip, "skip"), _dev(out["token_logp"], "token_logp"),
+        _dev(out.get("row_lse"), "row_lse"), _dev(out["path"], "path"), _dev(out["path_len"], "path_len"),
+        _dev(out["on_path"], "on_path"), _dev(out["utt_status"], "utt_status"), _dev(ws, "workspace"), ws.numel(),
+        _stream(), _opts(opts))
+    if rc != OK:
+        raise SsdError(rc, "ssd_verify_tree")
+    return out
+
+
+def _weights(weight: Optional[torch.Tensor], name: str, B: int, device):
+    """Address, stride and columns of [B, slots] weights."""
+    if weight is None:
+        return None, 0, 0
+    if weight.dtype != torch.float32 or weight.dim() != 2 or weight.shape[0] != B or \
+            (weight.shape[1] > 1 and weight.stride(1) != 1):
+        raise ValueError("%s must be float32 [B, slots] with contiguous rows" % name)
+    return _dev(weight, name), (weight.stride(0) if B > 1 else max(weight.stride(0), weight.shape[1])), weight.shape[1]
+
+
+def alloc_cache_append_outputs(B: int, device) -> Dict[str, torch.Tensor]:
+    return dict(new_len=torch.empty((B,), dtype=torch.int32, device=device),
+                utt_status=torch.empty((B,), dtype=torch.int32, device=device))
+
+
+def ssd_cache_append(tree_k: torch.Tensor, tree_v: torch.Tensor, tok_off: torch.Tensor, path: Optional[torch.Tensor],
+                     path_len: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, page_table: torch.Tensor,
+                     cache_len: torch.Tensor, weight: Optional[torch.Tensor] = None, out=None) -> Dict[str, torch.Tensor]:
+    """The accepted path's keys and values enter the cache, in place (the K/V of Eq. 7's verified prefix); path and
+    path_len as ssd_verify_tree leaves them, path None: an utterance's first path_len nodes.  weight [B, slots]
+    is set to 0 for the new slots.  Returns new_len, which is not cache_len, and utt_status."""
+    M, B = tree_k.shape[0], _nodes(tok_off, path, tree_k.shape[0])
+    if tree_k.dtype != k_cache.dtype or tree_v.dtype != k_cache.dtype:
+        raise TypeError("tree_k, tree_v and the cache must have one type")
+    for name, x in (("tree_k", tree_k), ("tree_v", tree_v)):
+        if x.dim() != 3 or x.shape[0] != M or x.shape[2] != k_cache.shape[3]:
+            raise ValueError("%s must be [M, heads, head_dim] like the cache" % name)
+    if path_len.dtype != torch.int32 or path_len.shape != (B,) or not path_len.is_contiguous():
+        raise TypeError("path_len must be a contiguous int32 [B]")
+    if out is None:
+        out = alloc_cache_append_outputs(B, k_cache.device)
+    rc = lib().ssd_cache_append(
+        _ref(_heads(tree_k, "tree_k")), _ref(_heads(tree_v, "tree_v")),
+        _ref(_kv_cache(k_cache, v_cache, page_table, cache_len, B)), _dev(tok_off, "tok_off"), _dev(path, "path"),
+        _dev(path_len, "path_len"), B, M, *_weights(weight, "weight", B, k_cache.device),
+        _dev(out["new_len"], "new_len"), _dev(out["utt_status"], "utt_status"), _stream())
+    if rc != OK:
+        raise SsdError(rc, "ssd_cache_append")
+    return out
+
+
+def alloc_cache_weights_outputs(B: int, device) -> Dict[str, torch.Tensor]:
+    return dict(utt_status=torch.empty((B,), dtype=torch.int32, device=device))
+
+
+def ssd_cache_weights(q: torch.Tensor, lse: torch.Tensor, k_cache: torch.Tensor, page_table: torch.Tensor,
+                      cache_len: torch.Tensor, tok_off: torch.Tensor, max_nodes: int, weight: torch.Tensor,
+                      use: Optional[torch.Tensor] = None, scale: Optional[float] = None, cap: float = 0.0,
+                      out=None) -> Dict[str, torch.Tensor]:
+    """Adds to weight [B, slots], in place, the attention weight that every cached slot receives from the
+    nodes with use != 0 (None: all), summed over their heads; lse as ssd_tree_attention returns it."""
+    M, B = q.shape[0], _nodes(tok_off, None, q.shape[0])
+    if q.dim() != 3 or q.dtype != k_cache.dtype or k_cache.dim() != 4 or k_cache.shape[3] != q.shape[2]:
+        raise ValueError("q must be [M, heads, head_dim] of the cache's type")
+    if lse.dtype != torch.float32 or lse.shape != q.shape[:2] or not lse.is_contiguous():
+        raise ValueError("lse must be a contiguous float32 [M, heads]")
+    if use is not None and (use.dtype != torch.uint8 or use.shape != (M,) or not use.is_contiguous()):
+        raise TypeError("use must be a contiguous uint8 [M]")
+    if out is None:
+        out = alloc_cache_weights_outputs(B, q.device)
+    rc = lib().ssd_cache_weights(
+        _ref(_heads(q, "q")), _dev(lse, "lse"), _ref(_kv_cache(k_cache, None, page_table, cache_len, B)),
+        _dev(tok_off, "tok_off"), B, M, max_nodes, q.shape[2] ** -0.5 if scale is None else scale, cap,
+        _dev(use, "use"), *_weights(weight, "weight", B, q.device), _dev(out["utt_status"], "utt_status"), _stream())
+    if rc != OK:
+        raise SsdError(rc, "ssd_cache_weights")
+    return out
+
+
+def alloc_cache_evict_outputs(B: int, budget: int, device) -> Dict[str, torch.Tensor]:
+    e = lambda shape, dt: torch.empty(shape, dtype=dt, device=device)
+    return dict(kept=e((B, budget), torch.int32), weight=e((B, budget), torch.float32),
+                new_len=e((B,), torch.int32), utt_status=e((B,), torch.int32))
+
+
+def ssd_cache_evict(k_cache: torch.Tensor, v_cache: torch.Tensor, page_table: torch.Tensor, cache_len: torch.Tensor,
+                    weight: torch.Tensor, budget: int, sink: int = 0, recent: int = 0, out=None) -> Dict[str, torch.Tensor]:
+    """Caches of more than `budget` slots keep the first `sink`, the last `recent` and the heaviest between, moved
+    down in place and in order.  Returns kept [B, budget], the kept slots' weight [B, budget], new_len and
+    utt_status."""
+    B = cache_len.shape[0]
+    if out is None:
+        out = alloc_cache_evict_outputs(B, budget, k_cache.device)
+    kept = out["kept"]
+    if kept.dtype != torch.int32 or kept.shape != (B, budget) or not kept.is_contiguous():
+        raise ValueError("kept must be a contiguous int32 [B, budget]")
+    w_out, out_stride, out_cols = _weights(out.get("weight"), "out['weight']", B, k_cache.device)
+    if w_out is not None and out_cols < budget:
+        raise ValueError("out['weight'] must have a column for every kept slot")
+    rc = lib().ssd_cache_evict(
+        _ref(_kv_cache(k_cache, v_cache, page_table, cache_len, B)), *_weights(weight, "weight", B, k_cache.device),
+        B, budget, sink, recent, _dev(kept, "kept"), w_out, out_stride, _dev(out["new_len"], "new_len"),
+        _dev(out["utt_status"], "utt_status"), _stream())
+    if rc != OK:
+        raise SsdError(rc, "ssd_cache_evict")
     return out
 
 

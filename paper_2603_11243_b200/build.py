@@ -11,7 +11,8 @@ LIB = os.path.join(HERE, "libssd.so")
 CALL = os.path.join(HERE, "_ssd_call.so")
 HEADER = os.path.join(os.path.dirname(HERE), "include", "ssd.h")
 SOURCES = ["ssd_api.cu", "ssd_ctc.cu", "ssd_verify.cu", "ssd_verify_static.cu", "ssd_decide.cu", "ssd_verify_ee.cu",
-           "ssd_readspan.cu", "ssd_tree.cu"]
+           "ssd_readspan.cu", "ssd_tree.cu", "ssd_cache.cu",
+           "ssd_cache_weights.cu"]
 CALL_SOURCE = os.path.join(CSRC, "ssd_call.cpp")
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "--use_fast_math=false", "-Xcompiler", "-fPIC", "-shared", "-cudart", "shared"]

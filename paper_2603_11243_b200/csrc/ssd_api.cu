@@ -207,6 +207,31 @@ int32_t ssd_verify(const void *logits, ssd_dtype dtype, int32_t V, int64_t ld,
                          token_logp, row_lse, accepted_len, all_accepted, utt_status, plan, L);
 }
 
+int32_t ssd_verify_tree(const void *logits, ssd_dtype dtype, int32_t V, int64_t ld,
+                        const int64_t *tok_off, const int32_t *draft_ids, const int32_t *parent,
+                        int32_t B, int64_t M, float tau_slm, const uint8_t *skip,
+                        float *token_logp, float *row_lse, int32_t *path, int32_t *path_len,
+                        uint8_t *on_path, uint32_t *utt_status,
+                        void *workspace, size_t workspace_bytes, void *stream,
+                        const ssd_launch_opts *opts) {
+    if (dtype != SSD_F32 && dtype != SSD_BF16) return SSD_ERR_DTYPE;
+    if (B < 0 || M < 0 || V < 1 || ld < V || (opts && opts->finish == 2)) return SSD_ERR_ARG;
+    if (!tok_off) return SSD_ERR_NULL;
+    if (M > 0 && (!logits || !draft_ids || !token_logp || !path || !on_path)) return SSD_ERR_NULL;
+    if (B > 0 && (!path_len || !utt_status)) return SSD_ERR_NULL;
+    const int es = dtype == SSD_F32 ? 4 : 2;
+    if (reinterpret_cast<uintptr_t>(logits) % es) return SSD_ERR_ALIGN;
+    VerifyPlan plan;
+    int rc = plan_for_query(B, M, V, dtype, opts, &plan, RowsAt{logits, ld, false, skip != nullptr});
+    if (rc != SSD_OK) return rc;
+    if (B > 0 && (!workspace || workspace_bytes < plan.workspace_bytes ||
+                  reinterpret_cast<uintptr_t>(workspace) % 256))
+        return SSD_ERR_WORKSPACE;
+    Launch L{static_cast<cudaStream_t>(stream), opts};
+    return launch_verify_tree(logits, dtype, V, ld, M, tok_off, draft_ids, parent, B, tau_slm, skip, workspace,
+                              token_logp, row_lse, path, path_len, on_path, utt_status, plan, L);
+}
+
 int32_t ssd_verify_shard(const void *logits, ssd_dtype dtype, int32_t V_local, int64_t ld,
                          int64_t col0, const int64_t *tok_off, const int32_t *draft_ids,
                          int32_t B, int64_t M, const uint8_t *skip, float *shard_stats,
@@ -395,6 +420,59 @@ int32_t ssd_tree_attention(const ssd_heads *q, const ssd_heads *tree_k, const ss
     if (B > 0 && !utt_status) return SSD_ERR_NULL;
     return launch_tree_attention(*q, *tree_k, *tree_v, *cache, tok_off, parent, B, M, max_nodes, scale, cap, *out, lse,
                                  utt_status, static_cast<cudaStream_t>(stream));
+}
+
+int32_t ssd_cache_append(const ssd_heads *tree_k, const ssd_heads *tree_v, const ssd_kv_cache *cache,
+                         const int64_t *tok_off, const int32_t *path, const int32_t *path_len,
+                         int32_t B, int64_t M, float *weight, int64_t weight_stride, int32_t weight_cols,
+                         int32_t *new_len, uint32_t *utt_status, void *stream) {
+    if (!tree_k || !tree_v || !cache || !tok_off) return SSD_ERR_NULL;
+    if (B < 0 || M < 0) return SSD_ERR_ARG;
+    int rc = check_cache(*cache, B, true);
+    for (const ssd_heads *x : {tree_k, tree_v})
+        if (rc == SSD_OK) rc = check_heads(*x, M);
+    if (rc != SSD_OK) return rc;
+    if (tree_k->heads != cache->heads || tree_v->heads != cache->heads) return SSD_ERR_ARG;
+    if (B > 0 && (!path_len || !new_len || !utt_status)) return SSD_ERR_NULL;
+    if (weight && (weight_cols < 0 || weight_stride < (B > 1 ? weight_cols : 0))) return SSD_ERR_ARG;
+    // other parts of an utterance's path may still be reading what the first one replaces
+    if (B > 0 && (new_len == cache->len || new_len == path_len)) return SSD_ERR_ARG;
+    return launch_cache_append(*tree_k, *tree_v, *cache, tok_off, path, path_len, B, M, weight, weight_stride, weight_cols,
+                               new_len, utt_status, static_cast<cudaStream_t>(stream));
+}
+
+int32_t ssd_cache_weights(const ssd_heads *q, const float *lse, const ssd_kv_cache *cache,
+                          const int64_t *tok_off, int32_t B, int64_t M, int32_t max_nodes,
+                          float scale, float cap, const uint8_t *use,
+                          float *weight, int64_t weight_stride, int32_t weight_cols,
+                          uint32_t *utt_status, void *stream) {
+    if (!q || !cache || !tok_off) return SSD_ERR_NULL;
+    if (B < 0 || M < 0 || M > INT32_MAX || max_nodes < 0 || !check_scores(scale, cap)) return SSD_ERR_ARG;
+    int rc = check_cache(*cache, B, false);
+    if (rc == SSD_OK) rc = check_heads(*q, M);
+    if (rc != SSD_OK) return rc;
+    if (q->heads % cache->heads || q->heads / cache->heads > 128) return SSD_ERR_ARG;
+    if (weight_cols < 0 || weight_stride < (B > 1 ? weight_cols : 0)) return SSD_ERR_ARG;
+    if (B > 0 && (!utt_status || (weight_cols > 0 && !weight))) return SSD_ERR_NULL;
+    if (M > 0 && !lse) return SSD_ERR_NULL;
+    return launch_cache_weights(*q, lse, *cache, tok_off, B, M, max_nodes, scale, cap, use, weight, weight_stride, weight_cols,
+                                utt_status, static_cast<cudaStream_t>(stream));
+}
+
+int32_t ssd_cache_evict(const ssd_kv_cache *cache, const float *weight, int64_t weight_stride,
+                        int32_t weight_cols, int32_t B, int32_t budget, int32_t sink, int32_t recent,
+                        int32_t *kept, float *weight_out, int64_t weight_out_stride,
+                        int32_t *new_len, uint32_t *utt_status, void *stream) {
+    if (!cache) return SSD_ERR_NULL;
+    if (B < 0 || budget < 0 || sink < 0 || recent < 0 || (int64_t)sink + recent > budget) return SSD_ERR_ARG;
+    int rc = check_cache(*cache, B, true);
+    if (rc != SSD_OK) return rc;
+    if (weight_cols < 0 || weight_stride < (B > 1 ? weight_cols : 0)) return SSD_ERR_ARG;
+    if (weight_out && weight_out_stride < (B > 1 ? budget : 0)) return SSD_ERR_ARG;
+    if (B > 0 && (!new_len || !utt_status || (budget > 0 && !kept) || (weight_cols > 0 && !weight))) return SSD_ERR_NULL;
+    if (B > 0 && (weight_out == weight && weight)) return SSD_ERR_ARG;
+    return launch_cache_evict(*cache, weight, weight_stride, weight_cols, B, budget, sink, recent, kept, weight_out,
+                              weight_out_stride, new_len, utt_status, static_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

@@ -543,6 +543,10 @@ struct RowsAt {
 };
 int plan_verify(int B, int64_t M, int V, ssd_dtype dtype, const ssd_launch_opts *opts,
                 const RowsAt &at, VerifyPlan *plan);
+int launch_verify_tree(const void *logits, ssd_dtype dtype, int V, int64_t ld, int64_t M, const int64_t *tok_off,
+                       const int32_t *draft_ids, const int32_t *parent, int B, float tau_slm, const uint8_t *skip,
+                       void *workspace, float *token_logp, float *row_lse, int32_t *path, int32_t *path_len,
+                       uint8_t *on_path, uint32_t *utt_status, const VerifyPlan &plan, const Launch &L);
 int launch_verify_shard(const void *logits, ssd_dtype dtype, int V_local, int64_t ld, int64_t M,
                         int64_t col0, const int64_t *tok_off, const int32_t *draft_ids, int B,
                         const uint8_t *skip, void *workspace, float *shard_stats,
@@ -600,5 +604,14 @@ cudaError_t ensure_dynamic_smem(const void *kernel, size_t bytes);
 int launch_tree_attention(const ssd_heads &q, const ssd_heads &tree_k, const ssd_heads &tree_v, const ssd_kv_cache &cache,
                           const int64_t *tok_off, const int32_t *parent, int B, int64_t M, int max_nodes, float scale,
                           float cap, const ssd_heads &out, float *lse, uint32_t *status, cudaStream_t stream);
+int launch_cache_append(const ssd_heads &tree_k, const ssd_heads &tree_v, const ssd_kv_cache &cache, const int64_t *tok_off,
+                        const int32_t *path, const int32_t *path_len, int B, int64_t M, float *weight,
+                        int64_t weight_stride, int weight_cols, int32_t *new_len, uint32_t *status, cudaStream_t stream);
+int launch_cache_weights(const ssd_heads &q, const float *lse, const ssd_kv_cache &cache, const int64_t *tok_off, int B,
+                         int64_t M, int max_nodes, float scale, float cap, const uint8_t *use, float *weight,
+                         int64_t weight_stride, int weight_cols, uint32_t *status, cudaStream_t stream);
+int launch_cache_evict(const ssd_kv_cache &cache, const float *weight, int64_t weight_stride, int weight_cols, int B, int budget,
+                       int sink, int recent, int32_t *kept, float *weight_out, int64_t out_stride, int32_t *new_len,
+                       uint32_t *status, cudaStream_t stream);
 
 }  // namespace ssd

@@ -66,6 +66,15 @@ __device__ __forceinline__ void tmem_ld32(uint32_t addr, float *r) {
           "=r"(u[24]), "=r"(u[25]), "=r"(u[26]), "=r"(u[27]), "=r"(u[28]), "=r"(u[29]), "=r"(u[30]), "=r"(u[31])
         : "r"(addr));
 }
+__device__ __forceinline__ void tmem_ld16(uint32_t addr, float *r) {
+    uint32_t *u = reinterpret_cast<uint32_t *>(r);
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]),
+          "=r"(u[8]), "=r"(u[9]), "=r"(u[10]), "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15])
+        : "r"(addr));
+}
 __device__ __forceinline__ void tmem_st32(uint32_t addr, const float *r) {
     const uint32_t *u = reinterpret_cast<const uint32_t *>(r);
     asm volatile(
@@ -208,5 +217,7 @@ __host__ __device__ inline TileAt paged_tile(const Paging &p, int len, int t) {
 // driver refused (or there is none); record_cuda_error has been called.
 bool encode_map(CUtensorMap *map, ssd_dtype dtype, const void *base, int rank, const uint64_t *dims,
                 const uint64_t *strides, const uint32_t *box);
+bool encode_rows(CUtensorMap *map, ssd_dtype dtype, const ssd_heads &x, int D, int64_t M, int box_heads, int box_rows);
+bool encode_cache(CUtensorMap *map, const ssd_kv_cache &c, const void *data, int box);
 
 }  // namespace ssd

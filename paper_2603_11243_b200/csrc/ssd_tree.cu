@@ -628,6 +628,7 @@ int launch_tree_attention(const ssd_heads &q, const ssd_heads &tree_k, const ssd
     p.paging = paging(cache.page_size);
     p.G = q.heads / cache.heads;
     p.npt = kTile / p.G;
+    if (p.npt > max_nodes) p.npt = max_nodes > 0 ? max_nodes : 1;      // no more of q is fetched than a tree can have
     const int D = cache.head_dim;
     if (M > 0) {
         if (!encode_rows(&p.q, cache.dtype, q, D, M, p.G, p.npt) || !encode_rows(&p.tree_k, cache.dtype, tree_k, D, M, 1, kTreeBox) ||

@@ -721,6 +721,140 @@ __global__ void __launch_bounds__(kFinishThreads) verify_finish_kernel(
     }
 }
 
+// ---- verification along a tree ------------------------------------------------------------------
+// One CTA per utterance, as verify_finish_kernel, but node i is judged by the row of the node it
+// continues: its logit there, and that row's pairs, are merged beside the pairs of its own row (which
+// its children are judged by), so no thread waits for another's.  Then one warp goes over the nodes 32
+// at a time in ascending order: a parent in an earlier block already knows its depth, one in the same
+// block is reached by five rounds of pointer doubling over the lanes.  A chain of 1,024 nodes is 32
+// blocks, some 5 us; trees of up to 64 nodes are two.
+constexpr int kTreeShared = 1024;        // nodes whose state is held in shared memory, not in `path`
+
+template <typename T, int G, int L>
+__global__ void __launch_bounds__(kFinishThreads) tree_finish_kernel(
+    const char *logits, int V, int64_t ld, int64_t M,
+    const int64_t *tok_off, const int32_t *draft_ids, const int32_t *parent,
+    float log_tau, int reject_none, int reject_all, const uint8_t *skip,
+    const float2 *partials, int P, float *__restrict__ token_logp, float *__restrict__ row_lse,
+    int32_t *path, int32_t *__restrict__ path_len, uint8_t *__restrict__ on_path,
+    uint32_t *__restrict__ utt_status, const unsigned long long *err_word, unsigned long long epoch) {
+    constexpr int ES = Elem<T>::kBytes;
+    __shared__ unsigned flags;
+    __shared__ int s_state[kTreeShared], s_up[kTreeShared];
+    __shared__ int best_depth, best_node;
+    pdl_launch_dependents();
+    const int b = blockIdx.x, tid = threadIdx.x, sub = tid % G, lane = tid & 31;
+    if (M == 0) pdl_wait();        // no streaming kernel of this call before this one
+    const int64_t i0 = load_input(tok_off + b), i1 = load_input(tok_off + b + 1);
+    const bool skipped = skip != nullptr && load_input(skip + b) != 0;
+    struct Node {
+        int up;                    // -1: none; -2: out of range
+        float x;
+        bool id_ok;
+    };
+    auto fetch = [&](int64_t r) {
+        Node d;
+        const int i = (int)(r - i0);
+        const int up = parent ? load_input(parent + r) : i - 1, id = load_input(draft_ids + r);
+        d.up = up < -1 || up >= i ? -2 : up;
+        d.id_ok = id >= 0 && id < V;
+        d.x = d.up >= 0 && d.id_ok ? Elem<T>::load_l2(logits + ((i0 + d.up) * ld + id) * ES) : 0.f;
+        return d;
+    };
+    Node node{-1, 0.f, true};
+    const int64_t first = skipped || sub != 0 ? -1 : ranges::row_of_utterance(i0, i1, M, tid / G);
+    if (first >= 0) node = fetch(first);
+    pdl_wait();
+    const unsigned long long err = *err_word;
+    const uint32_t internal = (err == epoch) ? (uint32_t)SSD_UTT_INTERNAL : 0u;
+    if (!ranges::rows_sound(i0, i1, M)) {
+        if (tid == 0) { path_len[b] = 0; utt_status[b] = SSD_UTT_BAD_OFFSETS | internal; }
+        return;
+    }
+    const int n = i1 - i0 > 0x7fffffff ? 0x7fffffff : (int)(i1 - i0);
+    if (tid == 0) { flags = 0; best_depth = 0; best_node = -1; }
+    __syncthreads();
+    const bool shared = n <= kTreeShared;
+    int *const state = shared ? s_state : path + i0;
+    if (!skipped) {
+        unsigned mine = 0;
+        for (int base = 0; base < n; base += kFinishThreads / G) {
+            const int i = base + tid / G;
+            const bool there = i < n;
+            const int64_t r = i0 + (there ? i : 0);
+            if (base > 0 && there && sub == 0) node = fetch(r);
+            int up = there ? node.up : -1;
+            up = __shfl_sync(0xffffffffu, up, lane / G * G);
+            const int64_t above = i0 + max(up, 0);
+            const float2 own = merge_partials<G, L>(partials + r * P, P, sub);
+            const float2 from = merge_partials<G, L>(partials + above * P, P, sub);
+            if (there && sub == 0) {
+                const float lse = own.x + logf(own.y);
+                if (!(fabsf(lse) < INFINITY)) mine |= SSD_UTT_NONFINITE;
+                bool good = node.up == -1;
+                float logp = 0.f;
+                if (node.up >= 0) {
+                    const RowDecision d = decide_row(node.x, from.x, logf(from.y), node.id_ok, log_tau, reject_none, reject_all);
+                    mine |= d.flags;
+                    logp = d.logp;
+                    good = !d.reject;
+                } else if (node.up == -2) {
+                    mine |= SSD_UTT_BAD_PARENT;
+                    logp = -INFINITY;
+                }
+                token_logp[r] = logp;
+                if (row_lse) row_lse[r] = lse;
+                state[i] = good ? node.up + 2 : 0;
+                if (shared) s_up[i] = max(node.up, -1);
+            }
+        }
+        if (mine) atomicOr(&flags, mine);
+        __syncthreads();
+        if (tid < 32) {
+            int deep = 0, at = -1;                       // of this lane's nodes
+            for (int base = 0; base < n; base += 32) {
+                const int i = base + lane;
+                const int code = i < n ? state[i] : 0, up = code - 2;
+                bool ok = code != 0;
+                int to = -1, count = 1;                  // nodes counted so far, and the lane they end at
+                if (ok && up >= base) to = up - base;
+                else if (ok && up >= 0) {
+                    const int above = state[up];
+                    ok = above > 0;
+                    count = above + 1;
+                }
+#pragma unroll
+                for (int round = 0; round < 5; ++round) {
+                    const int from = to < 0 ? lane : to;
+                    const int to2 = __shfl_sync(0xffffffffu, to, from), count2 = __shfl_sync(0xffffffffu, count, from);
+                    const bool ok2 = __shfl_sync(0xffffffffu, (int)ok, from) != 0;
+                    if (to >= 0) { ok = ok && ok2; count += count2; to = to2; }
+                }
+                const int depth = ok ? count : 0;
+                if (i < n) state[i] = depth;
+                if (depth > deep) { deep = depth; at = i; }
+                __syncwarp();
+            }
+            const int most = __reduce_max_sync(0xffffffffu, deep);
+            const int who = (int)__reduce_min_sync(0xffffffffu, deep == most && most > 0 ? (unsigned)at : 0x7fffffffu);
+            if (lane == 0) { best_depth = most; best_node = most > 0 ? who : -1; }
+        }
+        __syncthreads();
+    }
+    for (int i = tid; i < n; i += blockDim.x) { path[i0 + i] = -1; on_path[i0 + i] = 0; }
+    __syncthreads();
+    if (tid == 0) {
+        int j = best_node;
+        for (int k = best_depth - 1; k >= 0; --k) {
+            path[i0 + k] = j;
+            on_path[i0 + j] = 1;
+            j = shared ? s_up[j] : parent ? parent[i0 + j] : j - 1;
+        }
+        path_len[b] = best_depth;
+        utt_status[b] = flags | internal;
+    }
+}
+
 constexpr uint32_t kStatsInternal = 0x7fc0dead;   // in place of a row's maximum: a wait ran out
 
 // Vocabulary-parallel verification, per rank: for every row of a verified utterance the
@@ -1148,6 +1282,7 @@ template <template <int, int> class Pick> static auto pick_lanes(int P, int64_t 
 }
 template <typename T> struct FinishKernels {
     template <int G, int L> struct Verify { static auto kernel() { return &verify_finish_kernel<T, G, L>; } };
+    template <int G, int L> struct Tree { static auto kernel() { return &tree_finish_kernel<T, G, L>; } };
     template <int G, int L> struct Shard { static auto kernel() { return &shard_finish_kernel<T, G, L>; } };
 };
 
@@ -1288,6 +1423,32 @@ int launch_verify(const void *logits, ssd_dtype dtype, int V, int64_t ld, int64_
         static_cast<const unsigned long long *>(err_word), epoch);
     if (e != cudaSuccess) { record_cuda_error(e); return SSD_ERR_CUDA; }
     e = cudaGetLastError();
+    if (e != cudaSuccess) { record_cuda_error(e); return SSD_ERR_CUDA; }
+    return SSD_OK;
+}
+
+// Verification along a tree: the same streaming kernel, then the closing kernel that judges every node by its
+// parent's row.
+int launch_verify_tree(const void *logits, ssd_dtype dtype, int V, int64_t ld, int64_t M, const int64_t *tok_off,
+                       const int32_t *draft_ids, const int32_t *parent, int B, float tau_slm, const uint8_t *skip,
+                       void *workspace, float *token_logp, float *row_lse, int32_t *path, int32_t *path_len,
+                       uint8_t *on_path, uint32_t *utt_status, const VerifyPlan &plan, const Launch &L) {
+    if (B == 0) return SSD_OK;
+    unsigned long long *err_word = static_cast<unsigned long long *>(workspace);
+    float2 *partials = reinterpret_cast<float2 *>(static_cast<char *>(workspace) + partials_offset(B));
+    const unsigned long long epoch = next_epoch();
+    const int rc = launch_verify_rows(logits, dtype, V, ld, M, tok_off, B, skip, workspace, epoch, plan, L);
+    if (rc != SSD_OK) return rc;
+    const Threshold th = threshold_of(tau_slm);
+    const int P = pairs_per_row(plan);
+    cudaError_t e = launch_pdl(
+        dtype == SSD_F32 ? pick_lanes<FinishKernels<float>::Tree>(P, M / B)
+                         : pick_lanes<FinishKernels<bf16_t>::Tree>(P, M / B),
+        (unsigned)B, (unsigned)kFinishThreads, 0, L.stream,
+        static_cast<const char *>(logits), V, ld, M, tok_off, draft_ids, parent, th.log_tau,
+        th.reject_none, th.reject_all, skip, static_cast<const float2 *>(partials), P, token_logp, row_lse,
+        path, path_len, on_path, utt_status, static_cast<const unsigned long long *>(err_word), epoch);
+    if (e == cudaSuccess) e = cudaGetLastError();
     if (e != cudaSuccess) { record_cuda_error(e); return SSD_ERR_CUDA; }
     return SSD_OK;
 }

@@ -87,3 +87,51 @@ class Case:
                 out[lo + i] = torch.einsum("hl,lhd->hd", torch.softmax(x, -1), v.double().repeat_interleave(self.Hq // self.Hkv, 1))
                 lse[lo + i] = torch.logsumexp(x, -1)
         return out, lse
+
+
+def verify_tree(logits, off, ids, parent, tau, judged=None):
+    """token_logp, row_lse, path, path_len, on_path in 64 bits; logits [M, V] float64.  A node whose parent is out of
+    range is rejected.  judged: float32 log-likelihoods to take the decisions by, in float32, instead of these."""
+    M = logits.shape[0]
+    with np.errstate(all="ignore"):
+        top = logits.max(1, keepdims=True)
+        lse = (top + np.log(np.exp(logits - top).sum(1, keepdims=True)))[:, 0]
+    logp, path, on = np.zeros(M), np.full(M, -1, np.int32), np.zeros(M, np.uint8)
+    length = np.zeros(len(off) - 1, np.int32)
+    for b in range(len(off) - 1):
+        lo, n = off[b], off[b + 1] - off[b]
+        line = [None] * n
+        best = []
+        for i in range(n):
+            p = parent[lo + i]
+            if p == -1:
+                line[i] = [i]
+            elif not 0 <= p < i:
+                logp[lo + i] = -np.inf
+            else:
+                logp[lo + i] = logits[lo + p, ids[lo + i]] - lse[lo + p]
+                if judged is None:
+                    over = tau <= 0 or (tau < 1 and logp[lo + i] > math.log(tau))
+                else:
+                    over = tau <= 0 or (tau < 1 and judged[lo + i] > np.float32(math.log(np.float32(tau))))
+                if line[p] is not None and over:
+                    line[i] = line[p] + [i]
+            if line[i] is not None and len(line[i]) > len(best):
+                best = line[i]
+        length[b] = len(best)
+        path[lo:lo + len(best)] = best
+        on[lo + np.array(best, np.int64)] = 1
+    return logp, lse, path, length, on
+
+
+def planted(rng, off, parent, V, likely=0.75):
+    """Logits and ids whose nodes are clearly likely (p of 0.1 and more at up to three children) or at noise level."""
+    M = int(off[-1])
+    x = rng.standard_normal((M, V))
+    ids = np.zeros(M, np.int32)
+    for b in range(len(off) - 1):
+        for r in range(off[b], off[b + 1]):
+            ids[r] = rng.integers(0, V)
+            if parent[r] >= 0 and rng.random() < likely:
+                x[off[b] + parent[r], ids[r]] = math.log(V) + 2.0 + rng.random()
+    return x, ids
