@@ -617,10 +617,25 @@ def ssd_greedy_step(logits: torch.Tensor, V: Optional[int] = None, out=None,
 
 # ---- draft trees and their cache ---------------------------------------------------------------
 
+def _here(t: Optional[torch.Tensor], name: str):
+    """Address of a tensor on the current device, which is the one that the library launches on."""
+    p = _dev(t, name)
+    if t is not None and t.device.index != torch.cuda.current_device():
+        raise ValueError("%s is on %s, which is not the current device" % (name, t.device))
+    return p
+
+
+def _flat(t: Optional[torch.Tensor], name: str, dtype, n: int):
+    """Address of a contiguous [n] of a type, or None for None."""
+    if t is not None and (t.dtype != dtype or t.shape != (n,) or not t.is_contiguous()):
+        raise ValueError("%s must be a contiguous %s [%d]" % (name, dtype, n))
+    return _here(t, name)
+
+
 def _heads(x: torch.Tensor, name: str) -> Heads:
     if x.dim() != 3 or (x.shape[2] > 1 and x.stride(2) != 1):
         raise ValueError("%s must be [rows, heads, head_dim] with contiguous heads" % name)
-    return Heads(_dev(x, name), x.stride(0), x.stride(1), x.shape[1])
+    return Heads(_here(x, name), x.stride(0), x.stride(1), x.shape[1])
 
 
 def _kv_code(t: torch.Tensor) -> int:
@@ -645,10 +660,10 @@ def _kv_cache(k_cache: torch.Tensor, v_cache: Optional[torch.Tensor], page_table
     if cache_len.dim() != 1 or cache_len.shape[0] != B or (B > 1 and cache_len.stride(0) != 1):
         raise ValueError("cache_len must be a contiguous [B]")
     pages, page, heads, D = k_cache.shape
-    return KvCache(_dev(k_cache, "k_cache"), _dev(v_cache, "v_cache"), k_cache.stride(0), k_cache.stride(1),
+    return KvCache(_here(k_cache, "k_cache"), _here(v_cache, "v_cache"), k_cache.stride(0), k_cache.stride(1),
                    k_cache.stride(2), pages, page, heads, D, _kv_code(k_cache), page_table.shape[1],
-                   _dev(page_table, "page_table"), max(page_table.stride(0), page_table.shape[1]) if B <= 1 else page_table.stride(0),
-                   _dev(cache_len, "cache_len"))
+                   _here(page_table, "page_table"), max(page_table.stride(0), page_table.shape[1]) if B <= 1 else page_table.stride(0),
+                   _here(cache_len, "cache_len"))
 
 
 def _ref(x):
@@ -677,6 +692,14 @@ def ssd_tree_attention(q: torch.Tensor, tree_k: torch.Tensor, tree_v: torch.Tens
     (one layer of the pass that Section 2.2 verifies with).  q [M, Hq, D]; tree_k, tree_v [M, Hkv, D];
     k_cache, v_cache [pages, page_size, Hkv, D]; parent None: chains; scale None: D ** -0.5; scores capped
     at cap by a tanh where cap > 0.  Returns out [M, Hq, D], lse [M, Hq] and utt_status [B]."""
+    if out is not None:
+        rc = (_call or _native()).tree_attention(
+            q, tree_k, tree_v, k_cache, v_cache, page_table, cache_len, tok_off, max_nodes, parent,
+            q.shape[-1] ** -0.5 if scale is None else scale, cap, out)
+        if rc == OK:
+            return out
+        if rc is not None:
+            raise SsdError(rc, "ssd_tree_attention")
     M, B = q.shape[0], _nodes(tok_off, parent, q.shape[0])
     if tree_k.dtype != q.dtype or tree_v.dtype != q.dtype or k_cache.dtype != q.dtype:
         raise TypeError("q, tree_k, tree_v and the cache must have one type")
@@ -695,9 +718,9 @@ def ssd_tree_attention(q: torch.Tensor, tree_k: torch.Tensor, tree_v: torch.Tens
     cache = _kv_cache(k_cache, v_cache, page_table, cache_len, B)
     rc = lib().ssd_tree_attention(
         _ref(_heads(q, "q")), _ref(_heads(tree_k, "tree_k")), _ref(_heads(tree_v, "tree_v")), _ref(cache),
-        _dev(tok_off, "tok_off"), _dev(parent, "parent"), B, M, max_nodes,
-        q.shape[2] ** -0.5 if scale is None else scale, cap, _ref(_heads(o, "out")), _dev(lse, "lse"),
-        _dev(out["utt_status"], "utt_status"), _stream())
+        _here(tok_off, "tok_off"), _here(parent, "parent"), B, M, max_nodes,
+        q.shape[2] ** -0.5 if scale is None else scale, cap, _ref(_heads(o, "out")), _here(lse, "lse"),
+        _flat(out["utt_status"], "utt_status", torch.int32, B), _stream())
     if rc != OK:
         raise SsdError(rc, "ssd_tree_attention")
     return out
@@ -715,22 +738,24 @@ def ssd_verify_tree(logits: torch.Tensor, tok_off: torch.Tensor, draft_ids: torc
                     V: Optional[int] = None, out=None, opts: Optional[LaunchOpts] = None) -> Dict[str, torch.Tensor]:
     """Stage 2 along a draft tree (Eq. 5 on every path): logits row i is the LLM's output after node i;
     returns the nodes' log-likelihoods and the longest accepted path.  parent None: chains."""
+    if out is not None and opts is None:
+        rc = (_call or _native()).verify_tree(logits, tok_off, draft_ids, parent, tau_slm, skip, V, out)
+        if rc == OK:
+            return out
+        if rc is not None:
+            raise SsdError(rc, "ssd_verify_tree")
     M, ld = _rows_ld(logits)
     V = logits.shape[1] if V is None else V
     B = _nodes(tok_off, parent, M)
-    if draft_ids.dtype != torch.int32:
-        raise TypeError("draft_ids must be int32")
-    if skip is not None and skip.dtype != torch.uint8:
-        raise TypeError("skip must be uint8")
     code = _dtype_code(logits)
     if out is None:
         out = alloc_verify_tree_outputs(M, B, logits.device, ssd_verify_workspace_bytes(B, M, V, code, opts))
     ws = out["workspace"]
     rc = lib().ssd_verify_tree(
-        _dev(logits, "logits"), code, V, ld, _dev(tok_off, "tok_off"), _dev(draft_ids, "draft_ids"),
-        _dev(parent, "parent"), B, M, C.c_float(tau_slm), _dev(skip, "skip"), _dev(out["token_logp"], "token_logp"),
-        _dev(out.get("row_lse"), "row_lse"), _dev(out["path"], "path"), _dev(out["path_len"], "path_len"),
-        _dev(out["on_path"], "on_path"), _dev(out["utt_status"], "utt_status"), _dev(ws, "workspace"), ws.numel(),
+        _here(logits, "logits"), code, V, ld, _here(tok_off, "tok_off"), _flat(draft_ids, "draft_ids", torch.int32, M),
+        _here(parent, "parent"), B, M, C.c_float(tau_slm), _flat(skip, "skip", torch.uint8, B), _flat(out["token_logp"], "token_logp", torch.float32, M),
+        _flat(out.get("row_lse"), "row_lse", torch.float32, M), _flat(out["path"], "path", torch.int32, M), _flat(out["path_len"], "path_len", torch.int32, B),
+        _flat(out["on_path"], "on_path", torch.uint8, M), _flat(out["utt_status"], "utt_status", torch.int32, B), _here(ws, "workspace"), ws.numel(),
         _stream(), _opts(opts))
     if rc != OK:
         raise SsdError(rc, "ssd_verify_tree")
@@ -744,7 +769,7 @@ def _weights(weight: Optional[torch.Tensor], name: str, B: int, device):
     if weight.dtype != torch.float32 or weight.dim() != 2 or weight.shape[0] != B or \
             (weight.shape[1] > 1 and weight.stride(1) != 1):
         raise ValueError("%s must be float32 [B, slots] with contiguous rows" % name)
-    return _dev(weight, name), (weight.stride(0) if B > 1 else max(weight.stride(0), weight.shape[1])), weight.shape[1]
+    return _here(weight, name), (weight.stride(0) if B > 1 else max(weight.stride(0), weight.shape[1])), weight.shape[1]
 
 
 def alloc_cache_append_outputs(B: int, device) -> Dict[str, torch.Tensor]:
@@ -758,6 +783,13 @@ def ssd_cache_append(tree_k: torch.Tensor, tree_v: torch.Tensor, tok_off: torch.
     """The accepted path's keys and values enter the cache, in place (the K/V of Eq. 7's verified prefix); path and
     path_len as ssd_verify_tree leaves them, path None: an utterance's first path_len nodes.  weight [B, slots]
     is set to 0 for the new slots.  Returns new_len, which is not cache_len, and utt_status."""
+    if out is not None:
+        rc = (_call or _native()).cache_append(tree_k, tree_v, tok_off, path, path_len, k_cache, v_cache,
+                                                page_table, cache_len, weight, out)
+        if rc == OK:
+            return out
+        if rc is not None:
+            raise SsdError(rc, "ssd_cache_append")
     M, B = tree_k.shape[0], _nodes(tok_off, path, tree_k.shape[0])
     if tree_k.dtype != k_cache.dtype or tree_v.dtype != k_cache.dtype:
         raise TypeError("tree_k, tree_v and the cache must have one type")
@@ -770,9 +802,9 @@ def ssd_cache_append(tree_k: torch.Tensor, tree_v: torch.Tensor, tok_off: torch.
         out = alloc_cache_append_outputs(B, k_cache.device)
     rc = lib().ssd_cache_append(
         _ref(_heads(tree_k, "tree_k")), _ref(_heads(tree_v, "tree_v")),
-        _ref(_kv_cache(k_cache, v_cache, page_table, cache_len, B)), _dev(tok_off, "tok_off"), _dev(path, "path"),
-        _dev(path_len, "path_len"), B, M, *_weights(weight, "weight", B, k_cache.device),
-        _dev(out["new_len"], "new_len"), _dev(out["utt_status"], "utt_status"), _stream())
+        _ref(_kv_cache(k_cache, v_cache, page_table, cache_len, B)), _here(tok_off, "tok_off"), _here(path, "path"),
+        _here(path_len, "path_len"), B, M, *_weights(weight, "weight", B, k_cache.device),
+        _flat(out["new_len"], "new_len", torch.int32, B), _flat(out["utt_status"], "utt_status", torch.int32, B), _stream())
     if rc != OK:
         raise SsdError(rc, "ssd_cache_append")
     return out
@@ -788,6 +820,14 @@ def ssd_cache_weights(q: torch.Tensor, lse: torch.Tensor, k_cache: torch.Tensor,
                       out=None) -> Dict[str, torch.Tensor]:
     """Adds to weight [B, slots], in place, the attention weight that every cached slot receives from the
     nodes with use != 0 (None: all), summed over their heads; lse as ssd_tree_attention returns it."""
+    if out is not None:
+        rc = (_call or _native()).cache_weights(
+            q, lse, k_cache, page_table, cache_len, tok_off, max_nodes, weight, use,
+            q.shape[-1] ** -0.5 if scale is None else scale, cap, out)
+        if rc == OK:
+            return out
+        if rc is not None:
+            raise SsdError(rc, "ssd_cache_weights")
     M, B = q.shape[0], _nodes(tok_off, None, q.shape[0])
     if q.dim() != 3 or q.dtype != k_cache.dtype or k_cache.dim() != 4 or k_cache.shape[3] != q.shape[2]:
         raise ValueError("q must be [M, heads, head_dim] of the cache's type")
@@ -798,9 +838,9 @@ def ssd_cache_weights(q: torch.Tensor, lse: torch.Tensor, k_cache: torch.Tensor,
     if out is None:
         out = alloc_cache_weights_outputs(B, q.device)
     rc = lib().ssd_cache_weights(
-        _ref(_heads(q, "q")), _dev(lse, "lse"), _ref(_kv_cache(k_cache, None, page_table, cache_len, B)),
-        _dev(tok_off, "tok_off"), B, M, max_nodes, q.shape[2] ** -0.5 if scale is None else scale, cap,
-        _dev(use, "use"), *_weights(weight, "weight", B, q.device), _dev(out["utt_status"], "utt_status"), _stream())
+        _ref(_heads(q, "q")), _here(lse, "lse"), _ref(_kv_cache(k_cache, None, page_table, cache_len, B)),
+        _here(tok_off, "tok_off"), B, M, max_nodes, q.shape[2] ** -0.5 if scale is None else scale, cap,
+        _here(use, "use"), *_weights(weight, "weight", B, q.device), _flat(out["utt_status"], "utt_status", torch.int32, B), _stream())
     if rc != OK:
         raise SsdError(rc, "ssd_cache_weights")
     return out
@@ -817,6 +857,13 @@ def ssd_cache_evict(k_cache: torch.Tensor, v_cache: torch.Tensor, page_table: to
     """Caches of more than `budget` slots keep the first `sink`, the last `recent` and the heaviest between, moved
     down in place and in order.  Returns kept [B, budget], the kept slots' weight [B, budget], new_len and
     utt_status."""
+    if out is not None:
+        rc = (_call or _native()).cache_evict(k_cache, v_cache, page_table, cache_len, weight, budget, sink, recent,
+                                               out)
+        if rc == OK:
+            return out
+        if rc is not None:
+            raise SsdError(rc, "ssd_cache_evict")
     B = cache_len.shape[0]
     if out is None:
         out = alloc_cache_evict_outputs(B, budget, k_cache.device)
@@ -828,8 +875,8 @@ def ssd_cache_evict(k_cache: torch.Tensor, v_cache: torch.Tensor, page_table: to
         raise ValueError("out['weight'] must have a column for every kept slot")
     rc = lib().ssd_cache_evict(
         _ref(_kv_cache(k_cache, v_cache, page_table, cache_len, B)), *_weights(weight, "weight", B, k_cache.device),
-        B, budget, sink, recent, _dev(kept, "kept"), w_out, out_stride, _dev(out["new_len"], "new_len"),
-        _dev(out["utt_status"], "utt_status"), _stream())
+        B, budget, sink, recent, _here(kept, "kept"), w_out, out_stride, _flat(out["new_len"], "new_len", torch.int32, B),
+        _flat(out["utt_status"], "utt_status", torch.int32, B), _stream())
     if rc != OK:
         raise SsdError(rc, "ssd_cache_evict")
     return out

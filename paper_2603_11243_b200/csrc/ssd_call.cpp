@@ -90,7 +90,8 @@ PyObject *K_workspace, *K_frame_entropy, *K_frame_argmax, *K_frame_lse, *K_frame
     *K_draft_tokens, *K_draft_frames, *K_draft_len, *K_draft_full_len, *K_utt_max_entropy,
     *K_utt_status, *K_gate_accept, *K_max_entropy, *K_token_logp, *K_row_lse, *K_accepted_len,
     *K_all_accepted, *K_rows_read, *K_final_tokens, *K_final_len, *K_is_final, *K_ar_count, *K_ar_utt,
-    *K_ar_resume, *K_next_token, *K_next_logp, *K_row_status;
+    *K_ar_resume, *K_next_token, *K_next_logp, *K_row_status, *K_out, *K_lse, *K_path, *K_path_len,
+    *K_on_path, *K_new_len, *K_kept, *K_weight;
 
 struct Scratch {
     void *p;
@@ -332,10 +333,222 @@ PyObject *greedy_step(PyObject *, PyObject *const *a, Py_ssize_t n) {
     });
 }
 
+// ---- draft trees and their cache ----------------------------------------------------------------
+// the library launches on the current device
+void *here(const at::Tensor &t) {
+    void *p = address(t);
+    if (t.get_device() != c10::cuda::current_device()) throw Unhandled{};
+    return p;
+}
+ssd_dtype kv_type(const at::Tensor &t) {
+    if (t.scalar_type() == at::kBFloat16) return SSD_BF16;
+    if (t.scalar_type() == at::kHalf) return SSD_F16;
+    throw Unhandled{};
+}
+// [rows, heads, head_dim] with contiguous heads
+struct HeadsArg {
+    ssd_heads h;
+    int64_t rows, D;
+    ssd_dtype dtype;
+};
+HeadsArg heads(PyObject *o) {
+    const at::Tensor &t = tensor(o);
+    if (t.dim() != 3 || (t.size(2) > 1 && t.stride(2) != 1) || t.size(1) > INT_MAX) throw Unhandled{};
+    HeadsArg a;
+    a.dtype = kv_type(t);
+    a.h.data = here(t);
+    a.h.row_stride = t.stride(0);
+    a.h.head_stride = t.stride(1);
+    a.h.heads = (int32_t)t.size(1);
+    a.rows = t.size(0);
+    a.D = t.size(2);
+    return a;
+}
+// k_cache, v_cache (or null), page_table, cache_len of B utterances
+ssd_kv_cache kv_cache(PyObject *ko, PyObject *vo, PyObject *table_o, PyObject *len_o, int32_t B) {
+    const at::Tensor &k = tensor(ko), &table = typed(table_o, at::kInt), &len = typed(len_o, at::kInt);
+    if (k.dim() != 4 || (k.size(3) > 1 && k.stride(3) != 1)) throw Unhandled{};
+    ssd_kv_cache c;
+    c.dtype = kv_type(k);
+    c.k = here(k);
+    c.v = nullptr;
+    if (vo) {
+        const at::Tensor &v = tensor(vo);
+        if (v.scalar_type() != k.scalar_type() || v.dim() != 4) throw Unhandled{};
+        for (int i = 0; i < 4; ++i)
+            if (v.size(i) != k.size(i) || (k.size(i) > 1 && v.stride(i) != k.stride(i))) throw Unhandled{};
+        c.v = here(v);
+    }
+    for (int i = 0; i < 4; ++i)
+        if (k.size(i) > INT_MAX) throw Unhandled{};
+    c.page_stride = k.stride(0); c.slot_stride = k.stride(1); c.head_stride = k.stride(2);
+    c.pages = (int32_t)k.size(0); c.page_size = (int32_t)k.size(1); c.heads = (int32_t)k.size(2); c.head_dim = (int32_t)k.size(3);
+    if (table.dim() != 2 || table.size(0) != B || (table.size(1) > 1 && table.stride(1) != 1) || table.size(1) > INT_MAX) throw Unhandled{};
+    if (len.dim() != 1 || len.size(0) != B || (B > 1 && len.stride(0) != 1)) throw Unhandled{};
+    c.max_pages = (int32_t)table.size(1);
+    c.page_table = (const int32_t *)here(table);
+    c.table_stride = B > 1 ? table.stride(0) : std::max(table.stride(0), table.size(1));
+    c.len = (const int32_t *)here(len);
+    return c;
+}
+// a contiguous array of n values of a type, or null for None
+template <typename T> T *flat(PyObject *o, at::ScalarType type, int64_t n, bool nullable) {
+    if (nullable && (!o || o == Py_None)) return nullptr;
+    const at::Tensor &t = typed(o, type);
+    if (t.dim() != 1 || t.size(0) != n || !t.is_contiguous()) throw Unhandled{};
+    return (T *)here(t);
+}
+const int64_t *offsets(PyObject *o, int32_t &B) {
+    const at::Tensor &t = typed(o, at::kLong);
+    if (t.dim() != 1 || !t.is_contiguous()) throw Unhandled{};
+    B = utterances(t);
+    return (const int64_t *)here(t);
+}
+// [B, slots] of weights
+struct WeightArg {
+    float *p;
+    int64_t stride;
+    int32_t cols;
+};
+WeightArg weights(PyObject *o, int32_t B, bool nullable) {
+    if (nullable && (!o || o == Py_None)) return {nullptr, 0, 0};
+    const at::Tensor &t = typed(o, at::kFloat);
+    if (t.dim() != 2 || t.size(0) != B || (t.size(1) > 1 && t.stride(1) != 1) || t.size(1) > INT_MAX) throw Unhandled{};
+    return {(float *)here(t), B > 1 ? t.stride(0) : std::max(t.stride(0), t.size(1)), (int32_t)t.size(1)};
+}
+// a contiguous float32 [rows, heads], or null
+float *per_head(PyObject *o, int64_t rows, int64_t n, bool nullable) {
+    if (nullable && (!o || o == Py_None)) return nullptr;
+    const at::Tensor &t = typed(o, at::kFloat);
+    if (t.dim() != 2 || t.size(0) != rows || t.size(1) != n || !t.is_contiguous()) throw Unhandled{};
+    return (float *)here(t);
+}
+
+// tree_attention(q, tree_k, tree_v, k_cache, v_cache, page_table, cache_len, tok_off, max_nodes, parent, scale, cap, out)
+PyObject *tree_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded(n, 13, [&] {
+        int32_t B;
+        const int64_t *off = offsets(a[7], B);
+        const HeadsArg q = heads(a[0]), tk = heads(a[1]), tv = heads(a[2]);
+        const ssd_kv_cache c = kv_cache(a[3], a[4], a[5], a[6], B);
+        const int32_t max_nodes = int32(a[8]);
+        auto *parent = flat<const int32_t>(a[9], at::kInt, q.rows, true);
+        const float scale = number(a[10]), cap = number(a[11]);
+        need_dict(a[12]);
+        const HeadsArg o = heads(entry(a[12], K_out));
+        for (const HeadsArg *x : {&tk, &tv, &o})
+            if (x->dtype != q.dtype || x->rows != q.rows || x->D != q.D) throw Unhandled{};
+        if (c.dtype != q.dtype || c.head_dim != q.D || o.h.heads != q.h.heads) throw Unhandled{};
+        float *lse = per_head(entry(a[12], K_lse), q.rows, q.h.heads, true);
+        auto *us = flat<uint32_t>(entry(a[12], K_utt_status), at::kInt, B, false);
+        void *st = stream();
+        return [=] {
+            return ssd_tree_attention(&q.h, &tk.h, &tv.h, &c, off, parent, B, q.rows, max_nodes, scale, cap, &o.h, lse, us, st);
+        };
+    });
+}
+
+// verify_tree(logits, tok_off, draft_ids, parent, tau_slm, skip, V, out)
+PyObject *verify_tree(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded(n, 8, [&] {
+        const Rows x = rows(a[0], a[6]);
+        here(tensor(a[0]));
+        int32_t B;
+        const int64_t *off = offsets(a[1], B);
+        auto *ids = flat<const int32_t>(a[2], at::kInt, x.n, false);
+        auto *parent = flat<const int32_t>(a[3], at::kInt, x.n, true);
+        const float tau = number(a[4]);
+        auto *skip = flat<const uint8_t>(a[5], at::kByte, B, true);
+        PyObject *o = a[7];
+        need_dict(o);
+        auto *logp = flat<float>(entry(o, K_token_logp), at::kFloat, x.n, false);
+        auto *lse = flat<float>(entry(o, K_row_lse), at::kFloat, x.n, true);
+        auto *path = flat<int32_t>(entry(o, K_path), at::kInt, x.n, false);
+        auto *len = flat<int32_t>(entry(o, K_path_len), at::kInt, B, false);
+        auto *on = flat<uint8_t>(entry(o, K_on_path), at::kByte, x.n, false);
+        auto *us = flat<uint32_t>(entry(o, K_utt_status), at::kInt, B, false);
+        const Scratch ws = scratch(entry(o, K_workspace), true);
+        void *st = stream();
+        return [=] {
+            return ssd_verify_tree(x.p, x.dtype, (int32_t)x.V, x.ld, off, ids, parent, B, x.n, tau, skip, logp, lse, path, len, on, us,
+                                   ws.p, ws.bytes, st, nullptr);
+        };
+    });
+}
+
+// cache_append(tree_k, tree_v, tok_off, path, path_len, k_cache, v_cache, page_table, cache_len, weight, out)
+PyObject *cache_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded(n, 11, [&] {
+        int32_t B;
+        const int64_t *off = offsets(a[2], B);
+        const HeadsArg tk = heads(a[0]), tv = heads(a[1]);
+        auto *path = flat<const int32_t>(a[3], at::kInt, tk.rows, true);
+        auto *len = flat<const int32_t>(a[4], at::kInt, B, false);
+        const ssd_kv_cache c = kv_cache(a[5], a[6], a[7], a[8], B);
+        if (tv.rows != tk.rows || tk.D != c.head_dim || tv.D != c.head_dim || tk.dtype != c.dtype || tv.dtype != c.dtype) throw Unhandled{};
+        const WeightArg w = weights(a[9], B, true);
+        need_dict(a[10]);
+        auto *nl = flat<int32_t>(entry(a[10], K_new_len), at::kInt, B, false);
+        auto *us = flat<uint32_t>(entry(a[10], K_utt_status), at::kInt, B, false);
+        void *st = stream();
+        return [=] {
+            return ssd_cache_append(&tk.h, &tv.h, &c, off, path, len, B, tk.rows, w.p, w.stride, w.cols, nl, us, st);
+        };
+    });
+}
+
+// cache_weights(q, lse, k_cache, page_table, cache_len, tok_off, max_nodes, weight, use, scale, cap, out)
+PyObject *cache_weights(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded(n, 12, [&] {
+        int32_t B;
+        const int64_t *off = offsets(a[5], B);
+        const HeadsArg q = heads(a[0]);
+        const float *lse = per_head(a[1], q.rows, q.h.heads, false);
+        const ssd_kv_cache c = kv_cache(a[2], nullptr, a[3], a[4], B);
+        if (c.dtype != q.dtype || c.head_dim != q.D) throw Unhandled{};
+        const int32_t max_nodes = int32(a[6]);
+        const WeightArg w = weights(a[7], B, false);
+        auto *use = flat<const uint8_t>(a[8], at::kByte, q.rows, true);
+        const float scale = number(a[9]), cap = number(a[10]);
+        need_dict(a[11]);
+        auto *us = flat<uint32_t>(entry(a[11], K_utt_status), at::kInt, B, false);
+        void *st = stream();
+        return [=] {
+            return ssd_cache_weights(&q.h, lse, &c, off, B, q.rows, max_nodes, scale, cap, use, w.p, w.stride, w.cols, us, st);
+        };
+    });
+}
+
+// cache_evict(k_cache, v_cache, page_table, cache_len, weight, budget, sink, recent, out)
+PyObject *cache_evict(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded(n, 9, [&] {
+        const at::Tensor &len = typed(a[3], at::kInt);
+        if (len.dim() != 1 || len.size(0) > INT_MAX) throw Unhandled{};
+        const int32_t B = (int32_t)len.size(0);
+        const ssd_kv_cache c = kv_cache(a[0], a[1], a[2], a[3], B);
+        const WeightArg w = weights(a[4], B, false);
+        const int32_t budget = int32(a[5]), sink = int32(a[6]), recent = int32(a[7]);
+        need_dict(a[8]);
+        const at::Tensor &kept = typed(entry(a[8], K_kept), at::kInt);
+        if (kept.dim() != 2 || kept.size(0) != B || kept.size(1) != budget || !kept.is_contiguous()) throw Unhandled{};
+        auto *kp = (int32_t *)here(kept);
+        const WeightArg wo = weights(entry(a[8], K_weight), B, true);
+        if (wo.p && wo.cols < budget) throw Unhandled{};
+        auto *nl = flat<int32_t>(entry(a[8], K_new_len), at::kInt, B, false);
+        auto *us = flat<uint32_t>(entry(a[8], K_utt_status), at::kInt, B, false);
+        void *st = stream();
+        return [=] {
+            return ssd_cache_evict(&c, w.p, w.stride, w.cols, B, budget, sink, recent, kp, wo.p, wo.stride, nl, us, st);
+        };
+    });
+}
+
 #define SSD_METHOD(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {SSD_METHOD(ctc_draft), SSD_METHOD(gate_from_maxima), SSD_METHOD(verify),
                          SSD_METHOD(verify_early_exit), SSD_METHOD(verify_shard),
                          SSD_METHOD(verify_combine), SSD_METHOD(assemble), SSD_METHOD(greedy_step),
+                         SSD_METHOD(tree_attention), SSD_METHOD(verify_tree), SSD_METHOD(cache_append),
+                         SSD_METHOD(cache_weights), SSD_METHOD(cache_evict),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ssd_call", nullptr, -1, methods};
 // torch's C++ types change from release to release: the binding compares before the first call
@@ -351,7 +564,8 @@ PyMODINIT_FUNC PyInit__ssd_call() {
     SSD_KEY(max_entropy) SSD_KEY(token_logp) SSD_KEY(row_lse) SSD_KEY(accepted_len)
     SSD_KEY(all_accepted) SSD_KEY(rows_read) SSD_KEY(final_tokens) SSD_KEY(final_len)
     SSD_KEY(is_final) SSD_KEY(ar_count) SSD_KEY(ar_utt) SSD_KEY(ar_resume) SSD_KEY(next_token)
-    SSD_KEY(next_logp) SSD_KEY(row_status)
+    SSD_KEY(next_logp) SSD_KEY(row_status) SSD_KEY(out) SSD_KEY(lse) SSD_KEY(path)
+    SSD_KEY(path_len) SSD_KEY(on_path) SSD_KEY(new_len) SSD_KEY(kept) SSD_KEY(weight)
     PyObject *m = PyModule_Create(&module);
     if (m && PyModule_AddStringConstant(m, "built_for", kBuiltFor) < 0) {
         Py_DECREF(m);

@@ -168,3 +168,18 @@ def test_the_plain_reference_itself():
     assert torch.allclose(torch.einsum("hnl,ld->nhd", torch.softmax(x, -1), v), out, atol=1e-12)
     assert torch.allclose(torch.logsumexp(x, -1).t(), lse, atol=1e-12)
     assert tree_ref.lines([-1, 0, 0, 2, 9]) == [[0], [0, 1], [0, 2], [0, 2, 3], [4]]
+
+
+def test_the_native_marshalling_declines_what_is_not_plainly_fine():
+    call = ssd._native()
+    c = tree_ref.Case(1, [3, 2], [5, 6])
+    d = c.on("cpu")
+    out = ssd.alloc_tree_attention_outputs(5, 2, c.Hq, c.D, c.dtype, "cpu")
+    args = [d["q"], d["tk"], d["tv"], d["k"], d["v"], d["table"], d["lens"], d["off"], 3, d["parent"], 0.1, 0.0, out]
+    assert call.tree_attention(*args) is None and call.tree_attention(*args[:-1]) is None
+    assert call.verify_tree(torch.zeros(5, 9), d["off"], d["parent"], None, 0.1, None, None, out) is None
+    assert call.cache_append(d["tk"], d["tv"], d["off"], None, d["lens"], d["k"], d["v"], d["table"], d["lens"], None, {}) is None
+    assert call.cache_weights(d["q"], None, d["k"], d["table"], d["lens"], d["off"], 3, None, None, 0.1, 0.0, {}) is None
+    assert call.cache_evict(d["k"], d["v"], d["table"], d["lens"], None, 4, 0, 0, {}) is None
+    with pytest.raises(ValueError):
+        ssd.ssd_tree_attention(*args[:-1], out=out)
