@@ -22,7 +22,7 @@ namespace {
 
 using namespace tc;
 
-constexpr int kWarps = 10;
+constexpr int kWarps = 12;                // 8 of softmax, copies, products, and two that fill their group
 constexpr int kParents = 256;            // parents kept in shared memory; more are read from global
 constexpr int kTreeBox = 16;             // nodes that one copy brings
 constexpr int kMaxSplit = 8;
@@ -99,6 +99,29 @@ __device__ __forceinline__ int tree_tile_start(const Item &it, int t) { return (
 __device__ __forceinline__ int tile_valid(const AttnParams &p, const Item &it, int t) {
     if (t < it.tree_tiles) return min(kTile, it.last - tree_tile_start(it, t));
     return paged_tile(p.paging, it.len, t - it.tree_tiles).valid;
+}
+
+// The utterance's status, by one warp of its first item.
+__device__ __forceinline__ void report(const AttnParams &p, const Item &it, int item, int rank, bool failed, int lane) {
+    if (it.h == 0 && item % p.q_items == 0 && rank == 0) {
+        const int64_t i1 = p.off[it.b + 1];
+        uint32_t bits = 0;
+        if (it.i0 < 0 || i1 < it.i0 || i1 > p.M || i1 - it.i0 > p.max_nodes) bits |= SSD_UTT_BAD_OFFSETS;
+        if (p.len[it.b] != it.len) bits |= SSD_UTT_BAD_CACHE;
+        if (p.parent)
+            for (int j = lane; j < it.n; j += 32) {
+                const int up = p.parent[it.i0 + j];
+                if (up < -1 || up >= j) bits |= SSD_UTT_BAD_PARENT;
+            }
+        const int pages = it.n > 0 ? (int)(((int64_t)it.len + p.paging.page - 1) / p.paging.page) : 0;
+        for (int j = lane; j < pages; j += 32) {
+            const int id = p.table[it.b * p.table_stride + j];
+            if (id < 0 || id >= p.n_pages) bits |= SSD_UTT_BAD_CACHE;
+        }
+        bits = __reduce_or_sync(0xffffffffu, bits);
+        if (lane == 0 && !failed) p.status[it.b] = bits;
+    }
+    if (failed && lane == 0) p.status[it.b] = SSD_UTT_INTERNAL;
 }
 
 __device__ __forceinline__ int up_from(const AttnParams &p, const Item &it, const int16_t *parents, int j) {
@@ -193,7 +216,10 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
     const int T_ = it.work ? it.end - it.begin : 0;                 // key tiles of this CTA
     const int units = it.pair ? 2 * T_ : T_;                        // (stream, tile) pairs, in the order of their products
 
-    if (warp == 8 && T_ > 0) {
+    if (warp >= 8) {
+      // of the 168 registers a thread is launched with, softmax threads get 224 and these keep 56
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+      if (warp == 8 && T_ > 0) {
         // ---- copies -----------------------------------------------------------------------------
         if (lane == 0) {
             const int tiles = it.pair ? 2 : 1;
@@ -243,7 +269,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
             }
         }
         if (!ok) *failed = 1;
-    } else if (warp == 9 && T_ > 0) {
+      } else if (warp == 9 && T_ > 0) {
         // ---- products ---------------------------------------------------------------------------
         bool ok = mbar_wait_bounded(q_full, 0);
         auto scores = [&](int u) {
@@ -288,7 +314,19 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
             if (u + 2 < units) scores(u + 2);
         }
         if (!ok) *failed = 1;
-    } else if (warp < 8 && it.work) {
+      }
+      if (p.split > 1) { cluster_arrive(); cluster_wait(); cluster_arrive(); cluster_wait(); }
+      named_sync(0, kWarps * 32);
+      if (*failed) drain_after_error();
+      if (warp == 8) {
+        tc_fence_after();
+        tmem_free(tmem, 512);
+        report(p, it, item, rank, *failed != 0, lane);
+      }
+      return;
+    }
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
+    if (it.work) {
         // ---- softmax ------------------------------------------------------------------------------
         const int s = warp >> 2, quad = warp & 3, row = quad * 32 + lane;
         const int tile_q = it.pair ? s : 0;
@@ -351,7 +389,13 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
                     }
                     if (tree) {
                         const int t0 = tree_tile_start(it, t);
-                        while (walk >= t0) {
+                        if (!p.parent) {
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                const int left = node + 1 - t0 - j * 32;
+                                see[j] = left >= 32 ? 0xffffffffu : left > 0 ? (1u << left) - 1 : 0u;
+                            }
+                        } else while (walk >= t0) {
                             const int at = walk - t0;
                             if (at < kTile) {
 #pragma unroll
@@ -497,7 +541,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
         // ---- the cluster's partial results ------------------------------------------------------------
         cluster_arrive();
         cluster_wait();
-        if (it.work && warp < 8) {
+        if (it.work) {
             constexpr float kLift = Lag<T>::kLift;
             const float c = kCap ? kLog2e : p.scale * kLog2e;
             const int tiles = it.pair ? 2 : 1;
@@ -540,33 +584,8 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
         cluster_arrive();
         cluster_wait();
     }
-    __syncthreads();
-    if (*failed) drain_after_error();
-    __syncthreads();
-    if (warp == 8) {
-        tc_fence_after();
-        tmem_free(tmem, 512);
-        // ---- the utterance's status, by one warp of its first item -----------------------------------
-        if (it.h == 0 && item % p.q_items == 0 && rank == 0) {
-            const int64_t i1 = p.off[it.b + 1];
-            uint32_t bits = 0;
-            if (it.i0 < 0 || i1 < it.i0 || i1 > p.M || i1 - it.i0 > p.max_nodes) bits |= SSD_UTT_BAD_OFFSETS;
-            if (p.len[it.b] != it.len) bits |= SSD_UTT_BAD_CACHE;
-            if (p.parent)
-                for (int j = lane; j < it.n; j += 32) {
-                    const int up = p.parent[it.i0 + j];
-                    if (up < -1 || up >= j) bits |= SSD_UTT_BAD_PARENT;
-                }
-            const int pages = it.n > 0 ? (int)(((int64_t)it.len + p.paging.page - 1) / p.paging.page) : 0;
-            for (int j = lane; j < pages; j += 32) {
-                const int id = p.table[it.b * p.table_stride + j];
-                if (id < 0 || id >= p.n_pages) bits |= SSD_UTT_BAD_CACHE;
-            }
-            bits = __reduce_or_sync(0xffffffffu, bits);
-            if (lane == 0 && !*failed) p.status[it.b] = bits;
-        }
-        if (*failed && lane == 0) p.status[it.b] = SSD_UTT_INTERNAL;
-    }
+    tc_fence_before();
+    named_sync(0, kWarps * 32);
 }
 
 template <typename T, int D, bool kCap>
