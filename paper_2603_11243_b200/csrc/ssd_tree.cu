@@ -9,7 +9,7 @@
 // serves both) or, where the rows fill one tile or less, on one tile, whose key tiles then alternate
 // between two accumulators.  Either way there are two streams of (scores -> softmax -> product), so the
 // tensor cores work on one while the other's exponentials are taken: warps 0-3 and 4-7 hold one row a
-// thread, warp 8 issues the copies, warp 9 the products.  Scores and accumulators live in tensor
+// thread, warps 8 and 10 issue the copies, warp 9 the products.  Scores and accumulators live in tensor
 // memory; probabilities go back there in 16 bits, over the scores they came from, and are the first
 // operand of the second product.  Few rows and a long cache: the key tiles are split over a cluster
 // of CTAs, whose partial results meet in shared memory, so a call is one launch and needs no scratch.
@@ -22,7 +22,7 @@ namespace {
 
 using namespace tc;
 
-constexpr int kWarps = 12;                // 8 of softmax, copies, products, and two that fill their group
+constexpr int kWarps = 12;                // 8 of softmax, 2 of copies, 1 of products, and one that fills their group
 constexpr int kParents = 256;            // parents kept in shared memory; more are read from global
 constexpr int kTreeBox = 16;             // nodes that one copy brings
 constexpr int kMaxSplit = 8;
@@ -219,9 +219,10 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
     if (warp >= 8) {
       // of the 168 registers a thread is launched with, softmax threads get 224 and these keep 56
       asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-      if (warp == 8 && T_ > 0) {
-        // ---- copies -----------------------------------------------------------------------------
-        if (lane == 0) {
+      if ((warp == 8 || warp == 10) && T_ > 0) {
+        // ---- copies: queries and keys, and values, a warp each (it is the issue of many small copies that takes time) -----------------------------------------------------------------------------
+        const int kv = warp == 10;
+        if (!kv && lane == 0) {
             const int tiles = it.pair ? 2 : 1;
             mbar_arrive_expect_tx(q_full, tiles * S::kBlocks * p.G * p.npt * 128);
             for (int i = 0; i < tiles; ++i)
@@ -248,24 +249,20 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
             const int box = tree ? kTreeBox : p.paging.box, copies = (valid + box - 1) / box;
             const int t0 = tree ? tree_tile_start(it, t) : 0;
             const int slot0 = tree ? 0 : paged_tile(p.paging, it.len, t - it.tree_tiles).slot;
-            for (int kv = 0; kv < 2 && ok; ++kv) {
-                const int pos = 2 * (t - it.begin) + kv;
-                if (pos >= S::kSlots) ok = mbar_wait_bounded(slot_empty(pos % S::kSlots), (pos / S::kSlots - 1) & 1);
-                if (!ok) break;
-                const uint32_t bar = slot_full(pos % S::kSlots);
-                if (lane == 0) mbar_arrive_expect_tx(bar, copies * box * 128 * S::kBlocks);
-                __syncwarp();
-                for (int i = 0; i < copies; ++i) {
-                    const int page = __shfl_sync(0xffffffffu, id, p.paging.pages ? i : 0);
-                    if (lane < S::kBlocks) {
-                        const uint32_t dst = slot_at(pos) + lane * kBlockBytes + i * box * 128;
-                        if (tree)
-                            tma_load_3d(dst, kv ? &p.tree_v : &p.tree_k, lane * 64, it.h, (int)it.i0 + t0 + i * box, bar);
-                        else
-                            tma_load_4d(dst, kv ? &p.cache_v : &p.cache_k, lane * 64, it.h, p.paging.pages ? 0 : slot0 + i * box,
-                                        page, bar);
-                    }
-                }
+            const int pos = 2 * (t - it.begin) + kv;
+            if (pos >= S::kSlots) ok = mbar_wait_bounded(slot_empty(pos % S::kSlots), (pos / S::kSlots - 1) & 1);
+            if (!ok) break;
+            const uint32_t bar = slot_full(pos % S::kSlots);
+            if (lane == 0) mbar_arrive_expect_tx(bar, copies * box * 128 * S::kBlocks);
+            // a lane for every copy: of 64 columns and 8 rows at least, so 32 lanes are enough
+            const int i = lane / S::kBlocks, x = lane % S::kBlocks;
+            const int page = __shfl_sync(0xffffffffu, id, p.paging.pages ? i : 0);
+            if (i < copies) {
+                const uint32_t dst = slot_at(pos) + x * kBlockBytes + i * box * 128;
+                if (tree)
+                    tma_load_3d(dst, kv ? &p.tree_v : &p.tree_k, x * 64, it.h, (int)it.i0 + t0 + i * box, bar);
+                else
+                    tma_load_4d(dst, kv ? &p.cache_v : &p.cache_k, x * 64, it.h, p.paging.pages ? 0 : slot0 + i * box, page, bar);
             }
         }
         if (!ok) *failed = 1;
@@ -372,14 +369,11 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
                     if (j * 32 < valid) tmem_ld32(t_scores + j * 32, x + j * 32);
                     else {
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) x[j * 32 + i] = -INFINITY;
+                        for (int i = 0; i < 32; ++i) x[j * 32 + i] = 0.f;        // masked below
                     }
                 }
                 tmem_wait_ld();
-                if (kCap) {
-#pragma unroll
-                    for (int i = 0; i < kTile; ++i) x[i] = p.cap * tanhf(x[i] * (p.scale / p.cap));
-                }
+                if (kCap) cap_scores<kTile>(x, p.scale, p.cap);
                 if (tree || valid < kTile) {
                     uint32_t see[4];
 #pragma unroll
@@ -408,10 +402,13 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
 #pragma unroll
                     for (int i = 0; i < kTile; ++i) x[i] = see[i >> 5] >> (i & 31) & 1 ? x[i] : -INFINITY;
                 }
-                float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                float top[4] = {x[0], x[1], x[2], x[3]};
 #pragma unroll
-                for (int i = 0; i < kTile; ++i) top[i & 3] = fmaxf(top[i & 3], x[i]);
-                const float mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+                for (int i = 4; i < kTile; i += 8)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        top[k] = i + 4 + k < kTile ? fmaxf(fmaxf(top[k], x[i + k]), x[i + 4 + k]) : fmaxf(top[k], x[i + k]);
+                const float mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(fmaxf(top[2], top[3]), -INFINITY));
                 const bool grow = mx > m + lag || (m == -INFINITY && mx > m);
                 if (__any_sync(0xffffffffu, grow)) {
                     const float old = m;
@@ -431,22 +428,24 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
                     }
                 }
                 const float shift = (m == -INFINITY ? 0.f : m * c) - kLift;
-                float sum[4] = {0.f, 0.f, 0.f, 0.f};
+                float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     if (j * 32 < valid) {
                         uint32_t packed[16];
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
-                            const float lo = ex2(fmaf(x[j * 32 + 2 * i], c, -shift)), hi = ex2(fmaf(x[j * 32 + 2 * i + 1], c, -shift));
-                            sum[(2 * i) & 3] += lo;
-                            sum[(2 * i + 1) & 3] += hi;
-                            packed[i] = pack2<T>(lo, hi);
+                            float2 e = ffma2(make_float2(x[j * 32 + 2 * i], x[j * 32 + 2 * i + 1]), make_float2(c, c), make_float2(-shift, -shift));
+                            e.x = ex2(e.x);
+                            e.y = ex2(e.y);
+                            sum[i & 1] = fadd2(sum[i & 1], e);
+                            packed[i] = pack2<T>(e.x, e.y);
                         }
                         tmem_st16(t_scores + j * 16, packed);
                     }
                 }
-                l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                sum[0] = fadd2(sum[0], sum[1]);
+                l += sum[0].x + sum[0].y;
                 tmem_wait_st();
             }
             tc_fence_before();
