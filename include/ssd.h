@@ -442,13 +442,18 @@ typedef struct ssd_kv_cache {  /* k and v: [pages, page_size, heads, head_dim], 
  * cache is touched.  Keys and values of nodes that are not on a row's line, and what the cache
  * holds behind len, have no influence on it, NaN and infinities included.
  * utt_status [B] u32 (overwritten).  cache->k and ->v may be NULL with pages == 0.
+ * workspace: at least ssd_tree_attention_workspace_bytes(Hq, Hkv, head_dim, M, max_nodes) bytes, 256-byte
+ * aligned: results of items that several CTAs share.  It needs no clearing; two calls whose kernels
+ * may run at the same time must not share it.
  * Errors: SSD_ERR_NULL, SSD_ERR_ARG (sizes, head counts, head_dim, a scale that is not positive and
- * finite, a cap that is negative or not finite), SSD_ERR_DTYPE, SSD_ERR_ALIGN, SSD_ERR_CUDA.
+ * finite, a cap that is negative or not finite), SSD_ERR_DTYPE, SSD_ERR_ALIGN, SSD_ERR_WORKSPACE, SSD_ERR_CUDA.
  */
+size_t ssd_tree_attention_workspace_bytes(int32_t heads, int32_t kv_heads, int32_t head_dim, int64_t M, int32_t max_nodes);
 int32_t ssd_tree_attention(const ssd_heads *q, const ssd_heads *tree_k, const ssd_heads *tree_v,
                            const ssd_kv_cache *cache, const int64_t *tok_off, const int32_t *parent,
                            int32_t B, int64_t M, int32_t max_nodes, float scale, float cap,
-                           const ssd_heads *out, float *lse, uint32_t *utt_status, void *stream);
+                           const ssd_heads *out, float *lse, uint32_t *utt_status,
+                           void *workspace, size_t workspace_bytes, void *stream);
 
 /*
  * Verification of a draft tree: Eq. 5 along every path at once.  logits row i is the LLM's output

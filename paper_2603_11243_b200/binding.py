@@ -140,7 +140,10 @@ def lib():
         L.ssd_greedy_step.argtypes = [vp, C.c_int, i32, i64, i64, vp, vp, vp, vp, vp, C.c_size_t,
                                       vp, vp]
         L.ssd_tree_attention.restype = i32
-        L.ssd_tree_attention.argtypes = [vp, vp, vp, vp, vp, vp, i32, i64, i32, C.c_float, C.c_float, vp, vp, vp, vp]
+        L.ssd_tree_attention.argtypes = [vp, vp, vp, vp, vp, vp, i32, i64, i32, C.c_float, C.c_float, vp, vp, vp,
+                                         vp, C.c_size_t, vp]
+        L.ssd_tree_attention_workspace_bytes.restype = C.c_size_t
+        L.ssd_tree_attention_workspace_bytes.argtypes = [i32, i32, i32, i64, i32]
         L.ssd_verify_tree.restype = i32
         L.ssd_verify_tree.argtypes = [vp, C.c_int, i32, i64, vp, vp, vp, i32, i64, C.c_float, vp,
                                       vp, vp, vp, vp, vp, vp, vp, C.c_size_t, vp, vp]
@@ -678,10 +681,19 @@ def _nodes(tok_off: torch.Tensor, parent: Optional[torch.Tensor], M: int) -> int
     return tok_off.shape[0] - 1
 
 
-def alloc_tree_attention_outputs(M: int, B: int, heads: int, head_dim: int, dtype, device) -> Dict[str, torch.Tensor]:
+def ssd_tree_attention_workspace_bytes(heads: int, kv_heads: int, head_dim: int, M: int, max_nodes: int) -> int:
+    return int(lib().ssd_tree_attention_workspace_bytes(heads, kv_heads, head_dim, M, max_nodes))
+
+
+def alloc_tree_attention_outputs(M: int, B: int, heads: int, head_dim: int, dtype, device, kv_heads: int = 1,
+                                 max_nodes: Optional[int] = None) -> Dict[str, torch.Tensor]:
+    """kv_heads and max_nodes size the workspace: without them it is enough for any."""
+    ws = max([256] + [ssd_tree_attention_workspace_bytes(heads, kv, head_dim, M, M if max_nodes is None else max_nodes)
+                      for kv in range(kv_heads, heads + 1) if heads % kv == 0 and heads // kv <= 128])
     return dict(out=torch.empty((M, heads, head_dim), dtype=dtype, device=device),
                 lse=torch.empty((M, heads), dtype=torch.float32, device=device),
-                utt_status=torch.empty((B,), dtype=torch.int32, device=device))
+                utt_status=torch.empty((B,), dtype=torch.int32, device=device),
+                workspace=torch.empty((ws,), dtype=torch.uint8, device=device))
 
 
 def ssd_tree_attention(q: torch.Tensor, tree_k: torch.Tensor, tree_v: torch.Tensor, k_cache: torch.Tensor,
@@ -709,8 +721,8 @@ def ssd_tree_attention(q: torch.Tensor, tree_k: torch.Tensor, tree_v: torch.Tens
     if k_cache.dim() != 4 or k_cache.shape[3] != q.shape[2]:
         raise ValueError("the cache's heads are not as long as q's")
     if out is None:
-        out = alloc_tree_attention_outputs(M, B, q.shape[1], q.shape[2], q.dtype, q.device)
-    o, lse = out["out"], out.get("lse")
+        out = alloc_tree_attention_outputs(M, B, q.shape[1], q.shape[2], q.dtype, q.device, tree_k.shape[1], max_nodes)
+    o, lse, ws = out["out"], out.get("lse"), out["workspace"]
     if o.dtype != q.dtype or o.shape != q.shape:
         raise ValueError("out must have q's type and shape")
     if lse is not None and (lse.dtype != torch.float32 or lse.shape != q.shape[:2] or not lse.is_contiguous()):
@@ -720,7 +732,7 @@ def ssd_tree_attention(q: torch.Tensor, tree_k: torch.Tensor, tree_v: torch.Tens
         _ref(_heads(q, "q")), _ref(_heads(tree_k, "tree_k")), _ref(_heads(tree_v, "tree_v")), _ref(cache),
         _here(tok_off, "tok_off"), _here(parent, "parent"), B, M, max_nodes,
         q.shape[2] ** -0.5 if scale is None else scale, cap, _ref(_heads(o, "out")), _here(lse, "lse"),
-        _flat(out["utt_status"], "utt_status", torch.int32, B), _stream())
+        _flat(out["utt_status"], "utt_status", torch.int32, B), _here(ws, "workspace"), ws.numel(), _stream())
     if rc != OK:
         raise SsdError(rc, "ssd_tree_attention")
     return out

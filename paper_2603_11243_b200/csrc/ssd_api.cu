@@ -404,10 +404,18 @@ static int check_heads(const ssd_heads &x, int64_t M) {
 }
 static bool check_scores(float scale, float cap) { return scale > 0.f && scale < INFINITY && cap >= 0.f && cap < INFINITY; }
 
+size_t ssd_tree_attention_workspace_bytes(int32_t heads, int32_t kv_heads, int32_t head_dim, int64_t M, int32_t max_nodes) {
+    if (heads < 1 || kv_heads < 1 || heads % kv_heads || heads / kv_heads > 128 || (head_dim != 64 && head_dim != 128) || M < 0 ||
+        max_nodes < 0)
+        return 0;
+    return tree_attention_workspace_bytes(heads, kv_heads, head_dim, M, max_nodes);
+}
+
 int32_t ssd_tree_attention(const ssd_heads *q, const ssd_heads *tree_k, const ssd_heads *tree_v,
                            const ssd_kv_cache *cache, const int64_t *tok_off, const int32_t *parent,
                            int32_t B, int64_t M, int32_t max_nodes, float scale, float cap,
-                           const ssd_heads *out, float *lse, uint32_t *utt_status, void *stream) {
+                           const ssd_heads *out, float *lse, uint32_t *utt_status,
+                           void *workspace, size_t workspace_bytes, void *stream) {
     if (!q || !tree_k || !tree_v || !cache || !out || !tok_off) return SSD_ERR_NULL;
     if (B < 0 || M < 0 || M > INT32_MAX || max_nodes < 0 || !check_scores(scale, cap)) return SSD_ERR_ARG;
     int rc = check_cache(*cache, B, true);
@@ -418,8 +426,11 @@ int32_t ssd_tree_attention(const ssd_heads *q, const ssd_heads *tree_k, const ss
         tree_v->heads != cache->heads || out->heads != q->heads)
         return SSD_ERR_ARG;
     if (B > 0 && !utt_status) return SSD_ERR_NULL;
+    if (B > 0 && (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256 ||
+                  workspace_bytes < tree_attention_workspace_bytes(q->heads, cache->heads, cache->head_dim, M, max_nodes)))
+        return SSD_ERR_WORKSPACE;
     return launch_tree_attention(*q, *tree_k, *tree_v, *cache, tok_off, parent, B, M, max_nodes, scale, cap, *out, lse,
-                                 utt_status, static_cast<cudaStream_t>(stream));
+                                 utt_status, workspace, static_cast<cudaStream_t>(stream));
 }
 
 int32_t ssd_cache_append(const ssd_heads *tree_k, const ssd_heads *tree_v, const ssd_kv_cache *cache,

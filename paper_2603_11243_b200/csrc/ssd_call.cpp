@@ -440,10 +440,12 @@ PyObject *tree_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
             if (x->dtype != q.dtype || x->rows != q.rows || x->D != q.D) throw Unhandled{};
         if (c.dtype != q.dtype || c.head_dim != q.D || o.h.heads != q.h.heads) throw Unhandled{};
         float *lse = per_head(entry(a[12], K_lse), q.rows, q.h.heads, true);
+        const Scratch ws = scratch(entry(a[12], K_workspace), true);
         auto *us = flat<uint32_t>(entry(a[12], K_utt_status), at::kInt, B, false);
         void *st = stream();
         return [=] {
-            return ssd_tree_attention(&q.h, &tk.h, &tv.h, &c, off, parent, B, q.rows, max_nodes, scale, cap, &o.h, lse, us, st);
+            return ssd_tree_attention(&q.h, &tk.h, &tv.h, &c, off, parent, B, q.rows, max_nodes, scale, cap, &o.h, lse, us,
+                                      ws.p, ws.bytes, st);
         };
     });
 }

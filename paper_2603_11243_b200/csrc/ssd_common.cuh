@@ -603,7 +603,8 @@ cudaError_t ensure_dynamic_smem(const void *kernel, size_t bytes);
 // ---- draft trees and their cache (ssd_tree.cu, ssd_cache.cu) -------------------------------------
 int launch_tree_attention(const ssd_heads &q, const ssd_heads &tree_k, const ssd_heads &tree_v, const ssd_kv_cache &cache,
                           const int64_t *tok_off, const int32_t *parent, int B, int64_t M, int max_nodes, float scale,
-                          float cap, const ssd_heads &out, float *lse, uint32_t *status, cudaStream_t stream);
+                          float cap, const ssd_heads &out, float *lse, uint32_t *status, void *workspace, cudaStream_t stream);
+size_t tree_attention_workspace_bytes(int Hq, int Hkv, int D, int64_t M, int max_nodes);
 int launch_cache_append(const ssd_heads &tree_k, const ssd_heads &tree_v, const ssd_kv_cache &cache, const int64_t *tok_off,
                         const int32_t *path, const int32_t *path_len, int B, int64_t M, float *weight,
                         int64_t weight_stride, int weight_cols, int32_t *new_len, uint32_t *status, cudaStream_t stream);

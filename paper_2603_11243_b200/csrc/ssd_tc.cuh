@@ -113,6 +113,16 @@ template <typename T> __device__ __forceinline__ uint32_t instruction(uint32_t n
     return 1u << 4 | Format<T>::kCode << 7 | Format<T>::kCode << 10 | (b_mn_major ? 1u << 16 : 0u) | (n >> 3) << 17 |
            (uint32_t)(kTile >> 4) << 24;
 }
+// One thread of a converged warp.  Products are issued under this and with operands that are the same in
+// every lane as far as the compiler can see: under `lane == 0` each operand of each of them is moved to a uniform
+// register first, and eight products of 64 clocks took 1,000 to issue.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
+}
+// the value of lane 0, in every lane
+__device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, x, 0); }
 // d (+)= a . b; a and b in shared memory
 __device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
     asm volatile(
@@ -159,18 +169,25 @@ template <int N> __device__ __forceinline__ void cap_scores(float *x, float scal
 #pragma unroll
     for (int i = 0; i < N; ++i) most = fmax_nan(most, fabsf(x[i]));
     const bool all_small = __all_sync(0xffffffffu, most * r <= 0.5f);
-#pragma unroll
-    for (int i = 0; i < N; i += 2) {
-        const float2 v = make_float2(x[i], x[i + 1]), t = fmul2(v, v);
+    auto poly = [&](float2 v) {
+        const float2 t = fmul2(v, v);
         float2 q = ffma2(make_float2(c4, c4), t, make_float2(c3, c3));
         q = ffma2(q, t, make_float2(c2, c2));
         q = ffma2(q, t, make_float2(c1, c1));
         q = ffma2(q, t, make_float2(1.f, 1.f));
-        q = fmul2(q, fmul2(v, make_float2(scale, scale)));
-        if (all_small) {
+        return fmul2(q, fmul2(v, make_float2(scale, scale)));
+    };
+    if (all_small) {
+#pragma unroll
+        for (int i = 0; i < N; i += 2) {
+            const float2 q = poly(make_float2(x[i], x[i + 1]));
             x[i] = q.x;
             x[i + 1] = q.y;
-        } else {
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; i += 2) {
+            const float2 q = poly(make_float2(x[i], x[i + 1]));
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 const float y = x[i + k] * r;
@@ -187,17 +204,6 @@ __device__ __forceinline__ uint32_t unit_at(uint32_t tile, int row, int unit) {
 __device__ __forceinline__ void named_sync(int id, int threads) {
     asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
 }
-__device__ __forceinline__ float4 cluster_ld4(uint32_t a) {
-    float4 v;
-    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a) : "memory");
-    return v;
-}
-__device__ __forceinline__ float2 cluster_ld2(uint32_t a) {
-    float2 v;
-    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(a) : "memory");
-    return v;
-}
-
 // ---- the paged cache's tiles ------------------------------------------------------------------------
 // A tile is up to 128 consecutive slots that end within `pages` whole pages (pages of up to 64 slots,
 // a multiple of 8: as many as fit; other pages of up to 128: one) or within one page (larger pages).

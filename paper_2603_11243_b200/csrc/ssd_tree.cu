@@ -5,14 +5,19 @@
 // The query heads that share a kv head are rows of one product: a tile is 128 / G nodes by G heads, its
 // keys come 128 at a time, and the softmax is carried as a running maximum and sum per row.
 //
-// One CTA of ten warps works on one kv head and up to two tiles of queries (one pass over the keys
-// serves both) or, where the rows fill one tile or less, on one tile, whose key tiles then alternate
-// between two accumulators.  Either way there are two streams of (scores -> softmax -> product), so the
-// tensor cores work on one while the other's exponentials are taken: warps 0-3 and 4-7 hold one row a
-// thread, warps 8 and 10 issue the copies, warp 9 the products.  Scores and accumulators live in tensor
-// memory; probabilities go back there in 16 bits, over the scores they came from, and are the first
-// operand of the second product.  Few rows and a long cache: the key tiles are split over a cluster
-// of CTAs, whose partial results meet in shared memory, so a call is one launch and needs no scratch.
+// An item is one kv head of one utterance and up to two tiles of its queries; one pass over the item's keys
+// serves both tiles, or, where the rows fill one tile or less, its key tiles alternate between two
+// accumulators.  Either way there are two streams of (scores -> softmax -> product), so the tensor
+// cores work on one while the other's exponentials are taken: warps 0-3 and 4-7 hold one row a thread, warps
+// 8 and 10 issue the copies, warp 9 the products, and warp 11 keeps the work coming.
+// Scores and accumulators live in tensor memory; probabilities go back there in 16 bits, over the
+// scores they came from, and are the first operand of the second product.
+//
+// All items' key tiles form one line, which is cut into as many equal parts as there are multiprocessors: one
+// CTA each, whose pipeline runs on from item to item.  Lengths may be as ragged as they like, and few
+// items over long caches fill the device as well as many over short ones.  An item that a cut goes through
+// leaves partial results (unscaled sums, maxima and sums of probabilities, fp32) in the workspace, which a
+// closing kernel joins.
 #include <math.h>
 
 #include "ssd_tc.cuh"
@@ -22,10 +27,18 @@ namespace {
 
 using namespace tc;
 
-constexpr int kWarps = 12;                // 8 of softmax, 2 of copies, 1 of products, and one that fills their group
+constexpr int kWarps = 12;
 constexpr int kParents = 256;            // parents kept in shared memory; more are read from global
 constexpr int kTreeBox = 16;             // nodes that one copy brings
-constexpr int kMaxSplit = 8;
+
+// What a CTA leaves for the closing kernel: the part of an item that begins before it (`head`) and
+// that of one which goes on behind it (`tail`).
+struct Cut {
+    int32_t head;                        // 0: none; 1: goes on; 2: ends here
+    int32_t tail;                        // 1: there is one
+    int32_t b, h, node0, rows;           // the tail's item
+    int32_t first_b, last_b, failed;     // utterances this CTA worked on; whether a wait of its ran out
+};
 
 struct alignas(64) AttnParams {
     CUtensorMap q, tree_k, tree_v, cache_k, cache_v;
@@ -38,10 +51,14 @@ struct alignas(64) AttnParams {
     float *lse;
     uint32_t *status;
     int64_t table_stride, M;
-    int B, Hq, Hkv, G, npt, q_items, max_nodes, n_pages, max_pages, split;
+    Cut *cuts;                           // [grid]
+    float *parts;                        // [grid][2] x (rows pairs of maximum and sum, rows x D sums)
+    int part_rows;
+    int B, Hq, Hkv, G, npt, max_nodes, n_pages, max_pages;
     Paging paging;
     float scale, cap;
 };
+__host__ __device__ inline int64_t part_floats(int rows, int D) { return (int64_t)rows * (D + 2); }
 
 template <int D> struct Shape {
     static constexpr int kBlocks = D / 64;
@@ -49,85 +66,173 @@ template <int D> struct Shape {
     static constexpr int kSlots = D == 128 ? 5 : 8;
     static constexpr int kRing = 2 * kSlotBytes;                  // behind the two tiles of queries
     static constexpr int kMisc = kRing + kSlots * kSlotBytes;
-    static constexpr int kBars = kMisc;                           // q, full[], empty[], scores[2], probs[2], sums[2]
-    static constexpr int kNumBars = 1 + 2 * kSlots + 6;
-    static constexpr int kWords = kBars + kNumBars * 8;           // tmem address, failed, bad value seen
+    static constexpr int kBars = kMisc;     // full[], empty[], q full[2], q empty[2], scores[2], probs[2], sums[2], sums free
+    static constexpr int kNumBars = 2 * kSlots + 15;              // and segments full[2], empty[2]
+    static constexpr int kWords = kBars + kNumBars * 8;           // tmem address, failed, bad value seen [2]
     static constexpr int kMl = (kWords + 16 + 15) / 16 * 16;      // [2][128] running maximum and sum
     static constexpr int kParent = kMl + 2 * kTile * 8;
-    static constexpr int kBytes = kParent + kParents * 2;
-    static constexpr size_t kDynamic = kBytes;
+    static constexpr int kSegments = (kParent + kParents * 2 + 15) / 16 * 16;
+    static constexpr int kBytes = kSegments + 2 * 64;
     static constexpr int kO = 256;                                // tensor memory: scores at 0 and 128, sums here
 };
-static_assert(Shape<128>::kDynamic <= 232448, "shared memory");
-static_assert(2 * kTile * 128 * 4 <= Shape<128>::kSlots * Shape<128>::kSlotBytes, "partial results fit the ring");
-static_assert(2 * kTile * 64 * 4 <= Shape<64>::kSlots * Shape<64>::kSlotBytes, "partial results fit the ring");
+static_assert(Shape<128>::kBytes <= 232448, "shared memory");
 
-// What an item works on; the same in every thread.
-struct Item {
-    int64_t i0;          // first node of the utterance
-    int b, h, n, len;
-    int node0;           // first node of the item
-    int pair;            // two tiles of queries
-    int last;            // one past the last node that is a key
-    int tree_tiles, begin, end;    // of the key tiles, this CTA's
-    bool work;
+// ---- the line of key tiles and its cuts -----------------------------------------------------------
+// A tile costs as much as it has tiles of queries, an item 1 more for its end.
+struct Utterance {
+    int64_t i0;
+    int n, len, cache_tiles, q_items;
 };
-
-__device__ __forceinline__ Item item_of(const AttnParams &p, int item, int rank) {
-    Item it;
-    const int qi = item % p.q_items;
-    it.h = item / p.q_items % p.Hkv;
-    it.b = item / p.q_items / p.Hkv;
-    it.i0 = p.off[it.b];
-    const int64_t i1 = p.off[it.b + 1];
-    const bool ok = !(it.i0 < 0 || i1 < it.i0 || i1 > p.M || i1 - it.i0 > p.max_nodes);
-    it.n = ok ? (int)(i1 - it.i0) : 0;
+__device__ __forceinline__ Utterance utterance(const AttnParams &p, int b) {
+    Utterance u;
+    u.i0 = p.off[b];
+    const int64_t i1 = p.off[b + 1];
+    const int len = p.len[b];
+    const bool ok = !(u.i0 < 0 || i1 < u.i0 || i1 > p.M || i1 - u.i0 > p.max_nodes);
+    u.n = ok ? (int)(i1 - u.i0) : 0;
     const int64_t room = (int64_t)p.max_pages * p.paging.page;
-    it.len = min(max(p.len[it.b], 0), (int)min(room, (int64_t)INT32_MAX));
+    u.len = min(max(len, 0), (int)min(room, (int64_t)INT32_MAX));
+    u.cache_tiles = paged_tiles(p.paging, u.len);
+    u.q_items = (u.n + 2 * p.npt - 1) / (2 * p.npt);
+    return u;
+}
+struct Item {
+    int node0;           // its first node
+    int pair;            // 1: two tiles of queries
+    int last;            // one past the last node that is a key
+    int tree_tiles, tiles;
+};
+__device__ __forceinline__ Item item_of(const AttnParams &p, const Utterance &u, int qi) {
+    Item it;
     it.node0 = qi * 2 * p.npt;
-    it.work = it.node0 < it.n;
-    it.pair = it.n - it.node0 > p.npt;
-    it.last = min(it.n, it.node0 + 2 * p.npt);
+    it.pair = u.n - it.node0 > p.npt;
+    it.last = min(u.n, it.node0 + 2 * p.npt);
     it.tree_tiles = (it.last + kTile - 1) / kTile;
-    const int total = it.tree_tiles + paged_tiles(p.paging, it.len);
-    it.begin = (int)((int64_t)total * rank / p.split);
-    it.end = (int)((int64_t)total * (rank + 1) / p.split);
+    it.tiles = it.tree_tiles + u.cache_tiles;
     return it;
 }
-// The tree's own tiles come first, last nodes first: a thread walks its node's line upwards once.
-__device__ __forceinline__ int tree_tile_start(const Item &it, int t) { return (it.tree_tiles - 1 - t) * kTile; }
-__device__ __forceinline__ int tile_valid(const AttnParams &p, const Item &it, int t) {
-    if (t < it.tree_tiles) return min(kTile, it.last - tree_tile_start(it, t));
-    return paged_tile(p.paging, it.len, t - it.tree_tiles).valid;
+__device__ __forceinline__ int64_t cost(const Item &it) { return (int64_t)it.tiles * (1 + it.pair) + 1; }
+__device__ __forceinline__ int64_t cost(const AttnParams &p, const Utterance &u) {     // of one head
+    int64_t c = 0;
+    for (int qi = 0; qi < u.q_items; ++qi) c += cost(item_of(p, u, qi));
+    return c;
 }
 
-// The utterance's status, by one warp of its first item.
-__device__ __forceinline__ void report(const AttnParams &p, const Item &it, int item, int rank, bool failed, int lane) {
-    if (it.h == 0 && item % p.q_items == 0 && rank == 0) {
-        const int64_t i1 = p.off[it.b + 1];
-        uint32_t bits = 0;
-        if (it.i0 < 0 || i1 < it.i0 || i1 > p.M || i1 - it.i0 > p.max_nodes) bits |= SSD_UTT_BAD_OFFSETS;
-        if (p.len[it.b] != it.len) bits |= SSD_UTT_BAD_CACHE;
-        if (p.parent)
-            for (int j = lane; j < it.n; j += 32) {
-                const int up = p.parent[it.i0 + j];
-                if (up < -1 || up >= j) bits |= SSD_UTT_BAD_PARENT;
-            }
-        const int pages = it.n > 0 ? (int)(((int64_t)it.len + p.paging.page - 1) / p.paging.page) : 0;
-        for (int j = lane; j < pages; j += 32) {
-            const int id = p.table[it.b * p.table_stride + j];
-            if (id < 0 || id >= p.n_pages) bits |= SSD_UTT_BAD_CACHE;
-        }
-        bits = __reduce_or_sync(0xffffffffu, bits);
-        if (lane == 0 && !failed) p.status[it.b] = bits;
+// What a CTA works on next: tiles [begin, end) of an item.  One warp walks the line and keeps two of
+// these ahead of the others in shared memory.
+struct Segment {
+    int64_t i0;
+    int b, h, n, len;
+    int node0, pair, last, tree_tiles, tiles;
+    int begin, end;      // begin == end: no more
+    int pad[3];
+};
+static_assert(sizeof(Segment) == 64, "");
+
+// The CTA's part of the line [lo, hi), where in it the walk stands, and its next segment.
+struct Walk {
+    Utterance u;
+    Item it;
+    int64_t lo, hi, at;  // at: where the current item begins
+    int b, h, qi, begin, end;
+    __device__ __forceinline__ bool cut_item(const AttnParams &p) {
+        it = item_of(p, u, qi);
+        const int w = 1 + it.pair;
+        const int64_t from = lo - at, to = hi - at;      // tile k lies at at + k w
+        begin = from <= 0 ? 0 : (int)min((from + w - 1) / w, (int64_t)it.tiles);
+        end = to <= 0 ? 0 : (int)min((to + w - 1) / w, (int64_t)it.tiles);
+        return begin < end;
     }
-    if (failed && lane == 0) p.status[it.b] = SSD_UTT_INTERNAL;
+    __device__ __forceinline__ bool next(const AttnParams &p) {
+        do {
+            at += cost(it);
+            if (at >= hi) return false;
+            if (++qi == u.q_items) {
+                qi = 0;
+                if (++h == p.Hkv) {
+                    h = 0;
+                    do {
+                        if (++b >= p.B) return false;
+                        u = utterance(p, b);
+                    } while (u.n == 0);
+                }
+            }
+        } while (!cut_item(p));
+        return true;
+    }
+    // By one warp: costs[b] are the utterances' (of one head), the first `held` of them.
+    __device__ __forceinline__ bool first(const AttnParams &p, const int64_t *costs, int held, int lane) {
+        auto head_cost = [&](int i) { return i >= p.B ? 0 : i < held ? costs[i] : cost(p, utterance(p, i)); };
+        int64_t total = 0;
+        for (int i = lane; i < p.B; i += 32) total += head_cost(i);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+        total *= p.Hkv;
+        lo = total * blockIdx.x / gridDim.x;
+        hi = total * (blockIdx.x + 1) / gridDim.x;
+        if (lo >= hi) return false;
+        int64_t before = 0;
+        for (int i0 = 0; i0 < p.B; i0 += 32) {
+            const int64_t one = head_cost(i0 + lane), v = one * p.Hkv;
+            int64_t x = v;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int64_t y = __shfl_up_sync(0xffffffffu, x, o);
+                if (lane >= o) x += y;
+            }
+            const unsigned here = __ballot_sync(0xffffffffu, lo < before + x);
+            if (here) {
+                const int who = __ffs(here) - 1;         // lo lies in utterance i0 + who
+                b = i0 + who;
+                const int64_t each = __shfl_sync(0xffffffffu, one, who);
+                at = before + __shfl_sync(0xffffffffu, x - v, who);
+                u = utterance(p, b);
+                h = (int)((lo - at) / each);
+                at += h * each;
+                for (qi = 0; qi + 1 < u.q_items; ++qi) {
+                    const int64_t c = cost(item_of(p, u, qi));
+                    if (lo < at + c) break;
+                    at += c;
+                }
+                return cut_item(p) || next(p);
+            }
+            before += __shfl_sync(0xffffffffu, x, 31);
+        }
+        return false;
+    }
+};
+// The tree's own tiles come first, last nodes first: a thread walks its node's line upwards once.
+__device__ __forceinline__ int tree_tile_start(const volatile Segment &g, int t) { return (g.tree_tiles - 1 - t) * kTile; }
+__device__ __forceinline__ int tile_valid(const AttnParams &p, const volatile Segment &g, int t) {
+    if (t < g.tree_tiles) return min(kTile, g.last - tree_tile_start(g, t));
+    return paged_tile(p.paging, g.len, t - g.tree_tiles).valid;
 }
 
-__device__ __forceinline__ int up_from(const AttnParams &p, const Item &it, const int16_t *parents, int j) {
+// The status of utterance b, by one warp.
+__device__ __forceinline__ void report(const AttnParams &p, int b, int lane) {
+    const Utterance u = utterance(p, b);
+    const int64_t i1 = p.off[b + 1];
+    uint32_t bits = 0;
+    if (u.i0 < 0 || i1 < u.i0 || i1 > p.M || i1 - u.i0 > p.max_nodes) bits |= SSD_UTT_BAD_OFFSETS;
+    if (p.len[b] != u.len) bits |= SSD_UTT_BAD_CACHE;
+    if (p.parent)
+        for (int j = lane; j < u.n; j += 32) {
+            const int up = p.parent[u.i0 + j];
+            if (up < -1 || up >= j) bits |= SSD_UTT_BAD_PARENT;
+        }
+    const int pages = u.n > 0 ? (int)(((int64_t)u.len + p.paging.page - 1) / p.paging.page) : 0;
+    for (int j = lane; j < pages; j += 32) {
+        const int id = p.table[b * p.table_stride + j];
+        if (id < 0 || id >= p.n_pages) bits |= SSD_UTT_BAD_CACHE;
+    }
+    bits = __reduce_or_sync(0xffffffffu, bits);
+    if (lane == 0) p.status[b] = bits;
+}
+
+__device__ __forceinline__ int up_from(const AttnParams &p, int64_t i0, const int16_t *parents, int j) {
     if (!p.parent) return j - 1;
     if (j < kParents) return parents[j];
-    const int up = p.parent[it.i0 + j];
+    const int up = p.parent[i0 + j];
     return up < -1 || up >= j ? -1 : up;
 }
 
@@ -178,32 +283,40 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
     extern __shared__ __align__(1024) uint8_t base[];          // the swizzle is a function of the address
     const uint32_t smem = smem_u32(base);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int rank = blockIdx.x % p.split, item = blockIdx.x / p.split;
 
-    const uint32_t q_full = smem + S::kBars;
-    auto slot_full = [&](int i) { return smem + S::kBars + 8 + 8 * i; };
-    auto slot_empty = [&](int i) { return smem + S::kBars + 8 + 8 * (S::kSlots + i); };
-    const uint32_t more = smem + S::kBars + 8 + 16 * S::kSlots;
-    auto scores_full = [&](int s) { return more + 8 * s; };
-    auto probs_ready = [&](int s) { return more + 16 + 8 * s; };
-    auto sums_full = [&](int s) { return more + 32 + 8 * s; };
+    auto slot_full = [&](int pos) { return smem + S::kBars + 8 * (pos % S::kSlots); };
+    auto slot_empty = [&](int pos) { return smem + S::kBars + 8 * (S::kSlots + pos % S::kSlots); };
+    const uint32_t more = smem + S::kBars + 16 * S::kSlots;
+    auto q_full = [&](int i) { return more + 8 * i; };
+    auto q_empty = [&](int i) { return more + 16 + 8 * i; };
+    auto scores_full = [&](int s) { return more + 32 + 8 * s; };
+    auto probs_ready = [&](int s) { return more + 48 + 8 * s; };
+    auto sums_full = [&](int s) { return more + 64 + 8 * s; };
+    const uint32_t sums_free = more + 80;
+    auto segment_full = [&](int i) { return more + 88 + 8 * i; };
+    auto segment_empty = [&](int i) { return more + 104 + 8 * i; };
+    volatile Segment *const ring = reinterpret_cast<volatile Segment *>(base + S::kSegments);
     volatile uint32_t *const words = reinterpret_cast<volatile uint32_t *>(base + S::kWords);
-    volatile uint32_t *const failed = words + 1, *const seen = words + 2;
+    volatile uint32_t *const failed = words + 1;
     float2 *const ml = reinterpret_cast<float2 *>(base + S::kMl);
     int16_t *const parents = reinterpret_cast<int16_t *>(base + S::kParent);
     auto slot_at = [&](int pos) { return smem + S::kRing + (pos % S::kSlots) * S::kSlotBytes; };
 
     if (warp == 8) tmem_alloc(smem + S::kWords, 512);
     if (tid == 0) {
-        mbar_init(q_full, 1);
         for (int i = 0; i < S::kSlots; ++i) { mbar_init(slot_full(i), 1); mbar_init(slot_empty(i), 1); }
         for (int s = 0; s < 2; ++s) {
+            mbar_init(q_full(s), 1);
+            mbar_init(q_empty(s), 1);
             mbar_init(scores_full(s), 1);
             mbar_init(probs_ready(s), 4);
             mbar_init(sums_full(s), 1);
+            mbar_init(segment_full(s), 1);
+            mbar_init(segment_empty(s), 11);
         }
+        mbar_init(sums_free, 8);
         mbar_init_fence();
-        words[1] = words[2] = 0;
+        words[1] = words[2] = words[3] = 0;
     }
     tc_fence_before();
     __syncthreads();
@@ -211,155 +324,234 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
     pdl_launch_dependents();
     const uint32_t tmem = words[0];
     pdl_wait();
-
-    const Item it = item_of(p, item, rank);
-    const int T_ = it.work ? it.end - it.begin : 0;                 // key tiles of this CTA
-    const int units = it.pair ? 2 * T_ : T_;                        // (stream, tile) pairs, in the order of their products
+    // what the utterances cost, in front of the walk (in the queries' place, which are not there yet)
+    constexpr int kHeld = 2 * S::kSlotBytes / 8;
+    int64_t *const costs = reinterpret_cast<int64_t *>(base);
+    for (int b = tid; b < min(p.B, kHeld); b += kWarps * 32) costs[b] = cost(p, utterance(p, b));
+    fence_proxy_async();
+    __syncthreads();
+    // The i-th segment, read in place by whole warps: `take` waits for it, `give` hands its place back.
+    auto take = [&](int i, bool &ok) {
+        ok = ok && mbar_wait_bounded(segment_full(i & 1), i >> 1 & 1);
+        return ok && ring[i & 1].begin < ring[i & 1].end;
+    };
+    auto give = [&](int i) {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(segment_empty(i & 1));
+    };
 
     if (warp >= 8) {
-      // of the 168 registers a thread is launched with, softmax threads get 224 and these keep 56
-      asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-      if ((warp == 8 || warp == 10) && T_ > 0) {
-        // ---- copies: queries and keys, and values, a warp each (it is the issue of many small copies that takes time) -----------------------------------------------------------------------------
-        const int kv = warp == 10;
-        if (!kv && lane == 0) {
-            const int tiles = it.pair ? 2 : 1;
-            mbar_arrive_expect_tx(q_full, tiles * S::kBlocks * p.G * p.npt * 128);
-            for (int i = 0; i < tiles; ++i)
-                for (int x = 0; x < S::kBlocks; ++x)
-                    tma_load_3d(smem + i * S::kSlotBytes + x * kBlockBytes, &p.q, x * 64, it.h * p.G,
-                                (int)it.i0 + it.node0 + i * p.npt, q_full);
-        }
-        const int32_t *const table = p.table + it.b * p.table_stride;
-        const int page_count = p.paging.pages ? p.paging.pages : 1;
-        auto page_id = [&](int t) {                                  // lane i: the tile's i-th page
-            if (t < it.tree_tiles || t >= it.end || lane >= page_count) return 0;
-            const TileAt a = paged_tile(p.paging, it.len, t - it.tree_tiles);
-            if (a.page + lane >= p.max_pages) return p.n_pages;
-            const int id = table[a.page + lane];
-            return id < 0 || id >= p.n_pages ? p.n_pages : id;       // outside: the copy fills in zeros
-        };
-        int next = page_id(it.begin);
+        // of the 168 registers a thread is launched with, softmax threads get 224 and these keep 56
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         bool ok = true;
-        for (int t = it.begin; t < it.end && ok; ++t) {
-            const int id = next;
-            next = page_id(t + 1);
-            const bool tree = t < it.tree_tiles;
-            const int valid = tile_valid(p, it, t);
-            const int box = tree ? kTreeBox : p.paging.box, copies = (valid + box - 1) / box;
-            const int t0 = tree ? tree_tile_start(it, t) : 0;
-            const int slot0 = tree ? 0 : paged_tile(p.paging, it.len, t - it.tree_tiles).slot;
-            const int pos = 2 * (t - it.begin) + kv;
-            if (pos >= S::kSlots) ok = mbar_wait_bounded(slot_empty(pos % S::kSlots), (pos / S::kSlots - 1) & 1);
-            if (!ok) break;
-            const uint32_t bar = slot_full(pos % S::kSlots);
-            if (lane == 0) mbar_arrive_expect_tx(bar, copies * box * 128 * S::kBlocks);
-            // a lane for every copy: of 64 columns and 8 rows at least, so 32 lanes are enough
-            const int i = lane / S::kBlocks, x = lane % S::kBlocks;
-            const int page = __shfl_sync(0xffffffffu, id, p.paging.pages ? i : 0);
-            if (i < copies) {
-                const uint32_t dst = slot_at(pos) + x * kBlockBytes + i * box * 128;
-                if (tree)
-                    tma_load_3d(dst, kv ? &p.tree_v : &p.tree_k, x * 64, it.h, (int)it.i0 + t0 + i * box, bar);
-                else
-                    tma_load_4d(dst, kv ? &p.cache_v : &p.cache_k, x * 64, it.h, p.paging.pages ? 0 : slot0 + i * box, page, bar);
-            }
-        }
-        if (!ok) *failed = 1;
-      } else if (warp == 9 && T_ > 0) {
-        // ---- products ---------------------------------------------------------------------------
-        bool ok = mbar_wait_bounded(q_full, 0);
-        auto scores = [&](int u) {
-            const int s = u & 1, tile = it.pair ? u >> 1 : u, pos = 2 * tile, valid = tile_valid(p, it, it.begin + tile);
-            ok = ok && mbar_wait_bounded(slot_full(pos % S::kSlots), (pos / S::kSlots) & 1);
-            if (!ok) return;
-            tc_fence_after();
-            if (lane == 0) {
-                const uint32_t idesc = instruction<T>((valid + 15) / 16 * 16, false);
-                const uint64_t a = operand(smem + (it.pair ? s : 0) * S::kSlotBytes), k = operand(slot_at(pos));
-#pragma unroll
-                for (int x = 0; x < D / 16; ++x) {
-                    const int at = (x >> 2) * (kBlockBytes >> 4) + (x & 3) * 2;       // 16 columns = 32 bytes of a block's rows
-                    mma_ss(tmem + s * kTile, a + at, k + at, idesc, x > 0);
+        if (warp == 8 || warp == 10) {
+            // ---- copies: queries and keys, and values, a warp each (it is the issue of many small copies
+            // that takes time, so every lane issues one)
+            const int kv = warp == 10, page_count = p.paging.pages ? p.paging.pages : 1;
+            int pos = kv, used[2] = {0, 0}, buffer = 0;
+            for (int g = 0; take(g, ok); give(g++)) {
+                const volatile Segment &w = ring[g & 1];
+                const int begin = w.begin, end = w.end, tree_tiles = w.tree_tiles, h = w.h, len = w.len, i0 = (int)w.i0;
+                if (!kv) {
+                    for (int i = 0; i < 1 + w.pair && ok; ++i) {
+                        const int q = w.pair ? i : buffer;
+                        if (used[q] > 0) ok = mbar_wait_bounded(q_empty(q), (used[q] - 1) & 1);
+                        if (!ok) break;
+                        ++used[q];
+                        if (lane == 0) mbar_arrive_expect_tx(q_full(q), S::kBlocks * p.G * p.npt * 128);
+                        __syncwarp();
+                        if (lane < S::kBlocks)
+                            tma_load_3d(smem + q * S::kSlotBytes + lane * kBlockBytes, &p.q, lane * 64, h * p.G,
+                                        i0 + w.node0 + i * p.npt, q_full(q));
+                    }
+                    if (!w.pair) buffer ^= 1;
                 }
-                mma_commit(scores_full(s));
-                if (!it.pair || s) mma_commit(slot_empty(pos % S::kSlots));
+                const int32_t *const table = p.table + w.b * p.table_stride;
+                auto page_id = [&](int t) {                          // lane i: the tile's i-th page
+                    if (t < tree_tiles || t >= end || lane >= page_count) return 0;
+                    const TileAt a = paged_tile(p.paging, len, t - tree_tiles);
+                    if (a.page + lane >= p.max_pages) return p.n_pages;
+                    const int id = table[a.page + lane];
+                    return id < 0 || id >= p.n_pages ? p.n_pages : id;       // outside: the copy fills in zeros
+                };
+                int next = page_id(begin);
+                for (int t = begin; t < end && ok; ++t, pos += 2) {
+                    const int id = next;
+                    next = page_id(t + 1);
+                    const bool tree = t < tree_tiles;
+                    const int valid = tile_valid(p, w, t);
+                    const int box = tree ? kTreeBox : p.paging.box, copies = (valid + box - 1) / box;
+                    const int t0 = tree ? tree_tile_start(w, t) : 0;
+                    const int slot0 = tree ? 0 : paged_tile(p.paging, len, t - tree_tiles).slot;
+                    if (pos >= S::kSlots) ok = mbar_wait_bounded(slot_empty(pos), (pos / S::kSlots - 1) & 1);
+                    if (!ok) break;
+                    const uint32_t bar = slot_full(pos);
+                    if (lane == 0) mbar_arrive_expect_tx(bar, copies * box * 128 * S::kBlocks);
+                    // copies are of 64 columns and 8 rows at least, so 32 lanes are enough
+                    const int i = lane / S::kBlocks, x = lane % S::kBlocks;
+                    const int page = __shfl_sync(0xffffffffu, id, p.paging.pages ? i : 0);
+                    if (i < copies) {
+                        const uint32_t dst = slot_at(pos) + x * kBlockBytes + i * box * 128;
+                        if (tree)
+                            tma_load_3d(dst, kv ? &p.tree_v : &p.tree_k, x * 64, h, i0 + t0 + i * box, bar);
+                        else
+                            tma_load_4d(dst, kv ? &p.cache_v : &p.cache_k, x * 64, h, p.paging.pages ? 0 : slot0 + i * box,
+                                        page, bar);
+                    }
+                }
             }
-            __syncwarp();
-        };
-        auto values = [&](int u) {
-            const int s = u & 1, k = u >> 1, tile = it.pair ? k : u, pos = 2 * tile + 1, valid = tile_valid(p, it, it.begin + tile);
-            ok = ok && mbar_wait_bounded(probs_ready(s), k & 1) &&
-                 mbar_wait_bounded(slot_full(pos % S::kSlots), (pos / S::kSlots) & 1);
-            if (!ok) return;
-            tc_fence_after();
-            if (lane == 0) {
-                const uint32_t idesc = instruction<T>(D, true);
-                const uint64_t v = operand(slot_at(pos));
-                const int steps = (valid + 15) / 16;
-                for (int x = 0; x < steps; ++x)                                       // 16 keys = 2,048 bytes of a block
-                    mma_ts(tmem + S::kO + s * D, tmem + s * kTile + x * 8, v + x * (2048 >> 4), idesc, k > 0 || x > 0);
-                if (!it.pair || s) mma_commit(slot_empty(pos % S::kSlots));
-                if (u + 2 >= units) mma_commit(sums_full(s));
+        } else if (warp == 9) {
+            // ---- products -----------------------------------------------------------------------
+            const uint32_t tm = uniform(tmem);
+            int pos0 = 0, used[2] = {0, 0}, buffer = 0, done[2] = {0, 0};
+            for (int g = 0; take(g, ok); give(g++)) {
+                const volatile Segment &w = ring[g & 1];
+                const int begin = uniform(w.begin), pair = uniform(w.pair), tiles = uniform(w.end) - begin;
+                const int units = pair ? 2 * tiles : tiles;
+                for (int i = 0; i < 1 + pair && ok; ++i) {
+                    const int q = pair ? i : buffer;
+                    ok = mbar_wait_bounded(q_full(q), used[q]++ & 1);
+                }
+                // (stream, tile) pairs in the order of their products: u is of stream u & 1
+                auto groups = [&](int tile) { return uniform((tile_valid(p, w, begin + tile) + 15) >> 4); };     // of 16 keys
+                auto scores = [&](int u, int n16) {
+                    const int s = u & 1, tile = pair ? u >> 1 : u, pos = pos0 + 2 * tile, q = pair ? s : buffer;
+                    ok = ok && mbar_wait_bounded(slot_full(pos), (pos / S::kSlots) & 1);
+                    if (!ok) return;
+                    tc_fence_after();
+                    if (elect_one()) {
+                        const uint32_t idesc = instruction<T>(n16 * 16, false);
+                        const uint64_t a = operand(smem + q * S::kSlotBytes), k = operand(slot_at(pos));
+#pragma unroll
+                        for (int x = 0; x < D / 16; ++x) {
+                            const int at = (x >> 2) * (kBlockBytes >> 4) + (x & 3) * 2;   // 16 columns = 32 bytes of a block's rows
+                            mma_ss(tm + s * kTile, a + at, k + at, idesc, x > 0);
+                        }
+                        mma_commit(scores_full(s));
+                        if (!pair || s) mma_commit(slot_empty(pos));
+                        if (tile == tiles - 1) mma_commit(q_empty(q));
+                    }
+                    __syncwarp();
+                };
+                auto values = [&](int u, int n16) {
+                    const int s = u & 1, k = u >> 1, tile = pair ? k : u, pos = pos0 + 2 * tile + 1;
+                    ok = ok && mbar_wait_bounded(slot_full(pos), (pos / S::kSlots) & 1);
+                    if (u == 0 && g > 0) ok = ok && mbar_wait_bounded(sums_free, (g - 1) & 1);
+                    ok = ok && mbar_wait_bounded(probs_ready(s), (done[s] + k) & 1);
+                    if (!ok) return;
+                    tc_fence_after();
+                    if (elect_one()) {
+                        const uint32_t idesc = instruction<T>(D, true);
+                        const uint64_t v = operand(slot_at(pos));
+#pragma unroll
+                        for (int x = 0; x < kTile / 16; ++x)                              // 16 keys = 2,048 bytes of a block
+                            if (x < n16)
+                                mma_ts(tm + S::kO + s * D, tm + s * kTile + x * 8, v + x * (2048 >> 4), idesc, k > 0 || x > 0);
+                        if (!pair || s) mma_commit(slot_empty(pos));
+                        if (u + 2 >= units) mma_commit(sums_full(s));
+                    }
+                    __syncwarp();
+                };
+                // what a unit's products need is worked out before its wait
+                int n0 = groups(0), n1 = units > 1 ? groups(pair ? 0 : 1) : 0;
+                if (ok) scores(0, n0);
+                if (units > 1) scores(1, n1);
+                for (int u = 0; u < units && ok; ++u) {
+                    const int n2 = u + 2 < units ? groups(pair ? (u + 2) >> 1 : u + 2) : 0;
+                    values(u, n0);
+                    if (n2) scores(u + 2, n2);
+                    n0 = n1;
+                    n1 = n2;
+                }
+                done[0] += (units + 1) >> 1;
+                done[1] += units >> 1;
+                pos0 += 2 * tiles;
+                if (!pair) buffer ^= 1;
             }
-            __syncwarp();
-        };
-        scores(0);
-        if (units > 1) scores(1);
-        for (int u = 0; u < units && ok; ++u) {
-            values(u);
-            if (u + 2 < units) scores(u + 2);
+        } else {
+            // ---- the walk along the line ----------------------------------------------------------
+            Walk k;
+            bool more_work = k.first(p, costs, kHeld, lane);
+            // the costs are read: the queries may come (their warp waits for the first segment)
+            fence_proxy_async();
+            for (int g = 0; ok; ++g) {
+                if (g >= 2) ok = mbar_wait_bounded(segment_empty(g & 1), ((g >> 1) - 1) & 1);
+                if (!ok) break;
+                if (lane == 0) {
+                    volatile Segment &n = ring[g & 1];
+                    n.i0 = k.u.i0;
+                    n.b = k.b; n.h = k.h; n.n = k.u.n; n.len = k.u.len;
+                    n.node0 = k.it.node0; n.pair = k.it.pair; n.last = k.it.last; n.tree_tiles = k.it.tree_tiles; n.tiles = k.it.tiles;
+                    n.begin = more_work ? k.begin : 0;
+                    n.end = more_work ? k.end : 0;
+
+                    mbar_arrive(segment_full(g & 1));
+                }
+                __syncwarp();
+                if (!more_work) break;
+                more_work = k.next(p);
+            }
+            for (int b = blockIdx.x; b < p.B; b += gridDim.x) report(p, b, lane);
         }
         if (!ok) *failed = 1;
-      }
-      if (p.split > 1) { cluster_arrive(); cluster_wait(); cluster_arrive(); cluster_wait(); }
-      named_sync(0, kWarps * 32);
-      if (*failed) drain_after_error();
-      if (warp == 8) {
-        tc_fence_after();
-        tmem_free(tmem, 512);
-        report(p, it, item, rank, *failed != 0, lane);
-      }
-      return;
+        named_sync(0, kWarps * 32);
+        if (*failed) drain_after_error();
+        if (warp == 8) {
+            tc_fence_after();
+            tmem_free(tmem, 512);
+        }
+        return;
     }
     asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
-    if (it.work) {
-        // ---- softmax ------------------------------------------------------------------------------
-        const int s = warp >> 2, quad = warp & 3, row = quad * 32 + lane;
-        const int tile_q = it.pair ? s : 0;
-        const int first = it.node0 + tile_q * p.npt;                   // the tile's first node
-        const int rows = min(p.npt, it.n - first) * p.G;
+    // ---- softmax ------------------------------------------------------------------------------------
+    const int s = warp >> 2, quad = warp & 3, row = quad * 32 + lane;
+    const uint32_t lanes = (uint32_t)(quad * 32) << 16;
+    const uint32_t t_scores = tmem + s * kTile + lanes;
+    constexpr float kLift = Lag<T>::kLift;
+    const float c = kCap ? kLog2e : p.scale * kLog2e;
+    const float lag = Lag<T>::kLag / c;
+    const int tile_rows = p.npt * p.G;
+    bool ok = true;
+    int pos0 = 0, done = 0, closed[2] = {0, 0};
+    if (tid == 0) {
+        Cut none{};
+        none.first_b = 0x7fffffff;
+        none.last_b = -1;
+        p.cuts[blockIdx.x] = none;
+    }
+    for (int g = 0; take(g, ok); give(g++)) {
+        const volatile Segment &w = ring[g & 1];
+        const int pair = w.pair, begin = w.begin, tiles = w.end - begin;
+        const int tile_q = pair ? s : 0;
+        const int first = w.node0 + tile_q * p.npt;                 // the tile's first node
+        const int rows = min(p.npt, w.n - first) * p.G;
         const bool live = row < rows, busy = quad * 32 < rows;
-        const int node = first + row / p.G, head = it.h * p.G + row % p.G;
-        const uint32_t lanes = (uint32_t)(quad * 32) << 16;
-        const uint32_t t_scores = tmem + s * kTile + lanes, t_sums = tmem + S::kO + s * D + lanes;
-        const int count = T_ > 0 ? (it.pair ? T_ : (T_ - s + 1) >> 1) : 0;
-        constexpr float kLift = Lag<T>::kLift;
-        const float c = kCap ? kLog2e : p.scale * kLog2e;
-        const float lag = Lag<T>::kLag / c;
+        const int node = first + row / p.G, head = w.h * p.G + row % p.G;
+        const uint32_t t_sums = tmem + S::kO + s * D + lanes;
+        const int count = pair ? tiles : (tiles - s + 1) >> 1;
+        volatile uint32_t *const seen = words + 2 + (g & 1);
 
-        if (p.parent && it.begin < it.tree_tiles) {
-            for (int j = tid; j < min(it.last, kParents); j += 256) {
-                const int up = p.parent[it.i0 + j];
+        if (p.parent && begin < w.tree_tiles) {
+            for (int j = tid; j < min(w.last, kParents); j += 256) {
+                const int up = p.parent[w.i0 + j];
                 parents[j] = (int16_t)(up < -1 || up >= j ? -1 : up);
             }
             named_sync(1, 256);
         }
         int walk = live ? node : -1;
         float m = -INFINITY, l = 0.f;
-        bool ok = true;
         for (int k = 0; k < count; ++k) {
-            const int tile = it.pair ? k : 2 * k + s, t = it.begin + tile;
-            const bool tree = t < it.tree_tiles;
-            const int valid = tile_valid(p, it, t);
+            const int tile = pair ? k : 2 * k + s, t = begin + tile;
+            const bool tree = t < w.tree_tiles;
+            const int valid = tile_valid(p, w, t);
             if (tree || (valid & 15)) {
-                const int pos = 2 * tile + 1;
-                ok = ok && mbar_wait_bounded(slot_full(pos % S::kSlots), (pos / S::kSlots) & 1);
+                const int pos = pos0 + 2 * tile + 1;
+                ok = ok && mbar_wait_bounded(slot_full(pos), (pos / S::kSlots) & 1);
                 if (!ok) break;
                 clean_values<T>(slot_at(pos), row, valid, tree, D / 8, seen);
                 fence_proxy_async();
             }
-            ok = mbar_wait_bounded(scores_full(s), k & 1);
+            ok = mbar_wait_bounded(scores_full(s), (done + k) & 1);
             if (!ok) break;
             tc_fence_after();
             if (busy) {
@@ -382,7 +574,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
                         see[j] = tree ? 0u : left >= 32 ? 0xffffffffu : left > 0 ? (1u << left) - 1 : 0u;
                     }
                     if (tree) {
-                        const int t0 = tree_tile_start(it, t);
+                        const int t0 = tree_tile_start(w, t);
                         if (!p.parent) {
 #pragma unroll
                             for (int j = 0; j < 4; ++j) {
@@ -396,7 +588,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
                                 for (int j = 0; j < 4; ++j)
                                     if (at >> 5 == j) see[j] |= 1u << (at & 31);
                             }
-                            walk = up_from(p, it, parents, walk);
+                            walk = up_from(p, w.i0, parents, walk);
                         }
                     }
 #pragma unroll
@@ -417,13 +609,13 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
                     l *= f;
                     if (k > 0) {
 #pragma unroll
-                        for (int j = 0; j < D / 32; ++j) {
-                            float o[32];
-                            tmem_ld32(t_sums + j * 32, o);
+                        for (int j = 0; j < D / 16; ++j) {       // a few at a time: the scores fill the registers
+                            float o[16];
+                            tmem_ld16(t_sums + j * 16, o);
                             tmem_wait_ld();
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) o[i] *= f;
-                            tmem_st32(t_sums + j * 32, o);
+                            for (int i = 0; i < 16; ++i) o[i] *= f;
+                            tmem_st16(t_sums + j * 16, reinterpret_cast<const uint32_t *>(o));
                         }
                     }
                 }
@@ -452,44 +644,44 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
             __syncwarp();
             if (lane == 0) mbar_arrive(probs_ready(s));
         }
+        done += count;
+        pos0 += 2 * tiles;
         // ---- what came of it ------------------------------------------------------------------------
         ml[s * kTile + row] = make_float2(m, l);
-        const int other_count = T_ > 0 ? (T_ - (s ^ 1) + 1) >> 1 : 0;
-        if (count > 0) ok = ok && mbar_wait_bounded(sums_full(s), 0);
-        if (!it.pair && other_count > 0) ok = ok && mbar_wait_bounded(sums_full(s ^ 1), 0);
+        const bool any[2] = {true, pair || tiles > 1};                 // whether a stream had tiles
+        for (int i = 0; i < 2; ++i)
+            if (any[i]) {
+                if (!pair || i == s) ok = ok && mbar_wait_bounded(sums_full(i), closed[i] & 1);
+                ++closed[i];
+            }
         if (!ok) *failed = 1;
         named_sync(1, 256);
         tc_fence_after();
         const bool sick = *seen != 0;
-        // a pair of tiles: this stream's; else the two streams' sums of one tile, half the columns each
-        float w0 = 0.f, w1 = 0.f;              // what the own (pair) or stream 0's and stream 1's sums count
-        if (it.pair) {
-            w0 = count > 0 ? 1.f : 0.f;
-        } else {
+        // a pair of tiles: this stream's sums; else the two streams' of one tile, half the columns each
+        float w0 = 1.f, w1 = 0.f;
+        if (!pair) {
             const float2 a = ml[row], b = ml[kTile + row];
-            const bool has_b = T_ > 1;
-            m = has_b ? fmaxf(a.x, b.x) : a.x;
-            w0 = T_ > 0 && a.x > -INFINITY ? ex2((a.x - m) * c) : 0.f;
-            w1 = has_b && b.x > -INFINITY ? ex2((b.x - m) * c) : 0.f;
-            l = w0 * a.y + (has_b ? w1 * b.y : 0.f);
-            if (T_ == 0) l = 0.f;
+            m = any[1] ? fmaxf(a.x, b.x) : a.x;
+            w0 = a.x > -INFINITY ? ex2((a.x - m) * c) : 0.f;
+            w1 = any[1] && b.x > -INFINITY ? ex2((b.x - m) * c) : 0.f;
+            l = w0 * a.y + (any[1] ? w1 * b.y : 0.f);
         }
-        const int64_t out_at = (it.i0 + node) * p.out_row + head * p.out_head;
-        const float inv = p.split > 1 ? 1.f : l == 0.f ? 0.f : 1.f / l;
+        const bool whole = begin == 0 && w.end == w.tiles;
+        float *const part = p.parts + (2 * (int64_t)blockIdx.x + (begin == 0)) * part_floats(p.part_rows, D);
+        const int64_t out_at = (w.i0 + node) * p.out_row + head * p.out_head;
+        const float inv = !whole ? 1.f : l == 0.f ? 0.f : 1.f / l;
         const uint32_t own = tmem + S::kO + lanes;
         constexpr int kChunks = D / 32;
-        const int j0 = it.pair ? 0 : s * (kChunks / 2), j1 = it.pair ? kChunks : j0 + kChunks / 2;
+        const int j0 = pair ? 0 : s * (kChunks / 2), j1 = pair ? kChunks : j0 + kChunks / 2;
         if (busy) {
             for (int j = j0; j < j1; ++j) {
                 float o[32];
-                const bool any0 = it.pair ? count > 0 : T_ > 0, any1 = !it.pair && T_ > 1;
-                if (any0) {
-                    tmem_ld32(own + (it.pair ? s * D : 0) + j * 32, o);
-                    tmem_wait_ld();
-                }
+                tmem_ld32(own + (pair ? s * D : 0) + j * 32, o);
+                tmem_wait_ld();
 #pragma unroll
-                for (int i = 0; i < 32; ++i) o[i] = any0 ? o[i] * w0 * inv : 0.f;
-                if (any1) {
+                for (int i = 0; i < 32; ++i) o[i] = o[i] * w0 * inv;
+                if (!pair && any[1]) {
                     float o1[32];
                     tmem_ld32(own + D + j * 32, o1);
                     tmem_wait_ld();
@@ -498,8 +690,8 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
                 }
                 if (sick && live) {
                     // values that are not finite, to the nodes that see them
-                    for (int a = node; a >= 0; a = up_from(p, it, parents, a)) {
-                        const T *v = reinterpret_cast<const T *>(p.tree_v_at) + (it.i0 + a) * p.tree_row + it.h * p.tree_head + j * 32;
+                    for (int a = node; a >= 0; a = up_from(p, w.i0, parents, a)) {
+                        const T *v = reinterpret_cast<const T *>(p.tree_v_at) + (w.i0 + a) * p.tree_row + w.h * p.tree_head + j * 32;
 #pragma unroll
                         for (int i = 0; i < 32; ++i) {
                             const float y = (float)v[i];
@@ -508,7 +700,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
                     }
                 }
                 if (live) {
-                    if (p.split == 1) {
+                    if (whole) {
                         T *const to = reinterpret_cast<T *>(p.out) + out_at + j * 32;
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
@@ -516,86 +708,118 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
                                 make_uint4(pack2<T>(o[8 * i], o[8 * i + 1]), pack2<T>(o[8 * i + 2], o[8 * i + 3]),
                                            pack2<T>(o[8 * i + 4], o[8 * i + 5]), pack2<T>(o[8 * i + 6], o[8 * i + 7]));
                     } else {
-                        float4 *const to = reinterpret_cast<float4 *>(base + S::kRing) + (tile_q * kTile + row) * (D / 4);
+                        float4 *const to = reinterpret_cast<float4 *>(part + 2 * p.part_rows + (int64_t)(tile_q * tile_rows + row) * D + j * 32);
 #pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            to[(j * 8 + i) ^ (row & 15)] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                        for (int i = 0; i < 8; ++i) to[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
                     }
                 }
             }
         }
-        const float ln_lift = kLift * kLn2;
-        if (it.pair || s == 0) {
-            if (p.split == 1) {
-                if (live && p.lse)
-                    p.lse[(it.i0 + node) * p.Hq + head] = l == 0.f ? -INFINITY : (m * c) * kLn2 + (logf(l) - ln_lift);
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(sums_free);
+        if (live && (pair || s == 0)) {
+            if (!whole) reinterpret_cast<float2 *>(part)[tile_q * tile_rows + row] = make_float2(m, l);
+            else if (p.lse) p.lse[(w.i0 + node) * p.Hq + head] = l == 0.f ? -INFINITY : (m * c) * kLn2 + (logf(l) - kLift * kLn2);
+        }
+        if (tid == 0) {                              // nobody reads these in this grid
+            Cut &cut = p.cuts[blockIdx.x];
+            if (!whole) {
+                if (begin > 0) cut.head = w.end == w.tiles ? 2 : 1;
+                else {
+                    cut.tail = 1;
+                    cut.b = w.b; cut.h = w.h; cut.node0 = w.node0;
+                    cut.rows = min((1 + pair) * p.npt, w.n - w.node0) * p.G;
+                }
             }
+            if (g == 0) cut.first_b = w.b;
+            cut.last_b = w.b;
         }
-        if (p.split > 1) {
-            named_sync(1, 256);                         // everyone has read ml
-            if (it.pair || s == 0) ml[tile_q * kTile + row] = make_float2(m, l);
-        }
+        named_sync(1, 256);                          // everyone is done with ml, parents and seen
+        if (tid == 0) *seen = 0;
     }
-    if (p.split > 1) {
-        // ---- the cluster's partial results ------------------------------------------------------------
-        cluster_arrive();
-        cluster_wait();
-        if (it.work) {
-            constexpr float kLift = Lag<T>::kLift;
-            const float c = kCap ? kLog2e : p.scale * kLog2e;
-            const int tiles = it.pair ? 2 : 1;
-            const int nodes = min(it.n - it.node0, tiles * p.npt), all = nodes * p.G;
-            for (int e = rank * 256 + tid; e < all * (D / 4); e += p.split * 256) {
-                const int r = e / (D / 4), u = e - r * (D / 4);
-                const int tile_q = r / (p.npt * p.G), row = r - tile_q * p.npt * p.G;
-                const uint32_t ml_at = smem + S::kMl + (tile_q * kTile + row) * 8;
-                const uint32_t o_at = smem + S::kRing + ((tile_q * kTile + row) * (D / 4) + (u ^ (row & 15))) * 16;
-                float2 part[kMaxSplit];
-                float m = -INFINITY;
-#pragma unroll
-                for (int k = 0; k < kMaxSplit; ++k)
-                    if (k < p.split) {
-                        part[k] = cluster_ld2(cluster_address(ml_at, k));
-                        m = fmaxf(m, part[k].x);
-                    }
-                float l = 0.f;
-                float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-                for (int k = 0; k < kMaxSplit; ++k)
-                    if (k < p.split && part[k].x > -INFINITY) {
-                        const float w = ex2((part[k].x - m) * c);
-                        const float4 v = cluster_ld4(cluster_address(o_at, k));
-                        l = fmaf(w, part[k].y, l);
-                        o.x = fmaf(w, v.x, o.x); o.y = fmaf(w, v.y, o.y);
-                        o.z = fmaf(w, v.z, o.z); o.w = fmaf(w, v.w, o.w);
-                    } else if (k < p.split && part[k].y != part[k].y) {
-                        l = part[k].y;                   // NaN scores only
-                        o.x = o.y = o.z = o.w = l;
-                    }
-                const float inv = l == 0.f ? 0.f : 1.f / l;
-                const int64_t node = it.i0 + it.node0 + r / p.G;
-                const int head = it.h * p.G + r % p.G;
-                T *const to = reinterpret_cast<T *>(p.out) + node * p.out_row + head * p.out_head + u * 4;
-                *reinterpret_cast<uint2 *>(to) = make_uint2(pack2<T>(o.x * inv, o.y * inv), pack2<T>(o.z * inv, o.w * inv));
-                if (u == 0 && p.lse) p.lse[node * p.Hq + head] = l == 0.f ? -INFINITY : (m * c) * kLn2 + (logf(l) - kLift * kLn2);
-            }
-        }
-        cluster_arrive();
-        cluster_wait();
-    }
+    if (!ok) *failed = 1;
     tc_fence_before();
     named_sync(0, kWarps * 32);
+    if (tid == 0) p.cuts[blockIdx.x].failed = *failed != 0;
+}
+
+// Joins the parts of the item that begins in CTA blockIdx.x of the line and goes on behind it; four
+// blocks share its values.
+constexpr int kJoinBlocks = 4, kJoinThreads = 256;
+
+template <typename T, int D, bool kCap>
+__global__ void __launch_bounds__(kJoinThreads) tree_attention_join(const __grid_constant__ AttnParams p, int grid) {
+    pdl_enter();
+    const int first = blockIdx.x / kJoinBlocks;
+    const Cut cut = p.cuts[first];
+    if (cut.failed && blockIdx.x % kJoinBlocks == 0)
+        for (int b = cut.first_b + threadIdx.x; b <= cut.last_b; b += kJoinThreads) p.status[b] = SSD_UTT_INTERNAL;
+    if (!cut.tail) return;
+    int last = first + 1;                            // the CTA that the item ends in
+    while (last < grid && p.cuts[last].head != 2) ++last;
+    if (last == grid) return;
+    const float c = kCap ? kLog2e : p.scale * kLog2e;
+    const int64_t stride = 2 * part_floats(p.part_rows, D);
+    const float *const tail = p.parts + first * stride + part_floats(p.part_rows, D);
+    const int64_t i0 = p.off[cut.b];
+    for (int e = blockIdx.x % kJoinBlocks * kJoinThreads + threadIdx.x; e < cut.rows * (D / 4); e += kJoinBlocks * kJoinThreads) {
+        const int r = e / (D / 4), u = e - r * (D / 4);
+        float m = -INFINITY, l = 0.f;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int k = first; k <= last; ++k) {
+            if (k > first && k < last && p.cuts[k].head == 0) continue;      // too short a part for a tile
+            const float *const part = k == first ? tail : p.parts + k * stride;
+            const float2 a = reinterpret_cast<const float2 *>(part)[r];
+            const float4 v = reinterpret_cast<const float4 *>(part + 2 * p.part_rows + (int64_t)r * D)[u];
+            const float top = fmaxf(m, a.x);
+            const float f = m > -INFINITY ? ex2((m - top) * c) : 0.f, g = a.x > -INFINITY ? ex2((a.x - top) * c) : a.y;
+            // without a score (a.y == 0) nothing is added; with NaN scores alone (a.y is NaN) it is NaN
+            l = fmaf(l, f, a.x > -INFINITY ? g * a.y : a.y);
+            o.x = fmaf(o.x, f, g * v.x); o.y = fmaf(o.y, f, g * v.y);
+            o.z = fmaf(o.z, f, g * v.z); o.w = fmaf(o.w, f, g * v.w);
+            m = top;
+        }
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        const int64_t node = i0 + cut.node0 + r / p.G;
+        const int head = cut.h * p.G + r % p.G;
+        T *const to = reinterpret_cast<T *>(p.out) + node * p.out_row + head * p.out_head + u * 4;
+        *reinterpret_cast<uint2 *>(to) = make_uint2(pack2<T>(o.x * inv, o.y * inv), pack2<T>(o.z * inv, o.w * inv));
+        if (u == 0 && p.lse) p.lse[node * p.Hq + head] = l == 0.f ? -INFINITY : (m * c) * kLn2 + (logf(l) - Lag<T>::kLift * kLn2);
+    }
 }
 
 template <typename T, int D, bool kCap>
-int launch(const AttnParams &p, int64_t grid, cudaStream_t stream) {
+int launch(const AttnParams &p, int grid, cudaStream_t stream) {
     auto kernel = tree_attention<T, D, kCap>;
-    cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void *>(kernel), Shape<D>::kDynamic);
+    cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void *>(kernel), Shape<D>::kBytes);
+    if (e == cudaSuccess) e = launch_pdl(kernel, (unsigned)grid, kWarps * 32u, (size_t)Shape<D>::kBytes, stream, p);
     if (e == cudaSuccess)
-        e = launch_clusters(kernel, (unsigned)p.split, (unsigned)grid, kWarps * 32u, Shape<D>::kDynamic, stream, p);
+        e = launch_pdl(tree_attention_join<T, D, kCap>, (unsigned)(grid * kJoinBlocks), (unsigned)kJoinThreads, 0, stream, p, grid);
     if (e == cudaSuccess) e = cudaGetLastError();
     if (e != cudaSuccess) { record_cuda_error(e); return SSD_ERR_CUDA; }
     return SSD_OK;
+}
+
+struct AttnPlan {
+    int npt, part_rows, grid;
+    size_t cuts_bytes, bytes;
+};
+// grid: a CTA per multiprocessor, or per tile where there cannot be that many
+AttnPlan attention_plan(int Hq, int Hkv, int D, int64_t M, int max_nodes, int B, int64_t room, int sms) {
+    AttnPlan a;
+    const int G = Hq / Hkv;
+    if (max_nodes > M) max_nodes = (int)M;
+    a.npt = kTile / G;
+    if (a.npt > max_nodes) a.npt = max_nodes > 0 ? max_nodes : 1;      // no more of q is fetched than a tree can have
+    a.part_rows = ((max_nodes > a.npt ? 2 : 1) * a.npt * G + 3) / 4 * 4;      // sums begin on 16 bytes
+    const int64_t items = (int64_t)B * Hkv * ((max_nodes + 2 * a.npt - 1) / (2 * a.npt));
+    const int64_t tiles = (max_nodes + kTile - 1) / kTile + (room + 7) / 8;      // a tile has 8 slots at least, or a page
+    a.grid = items < sms && items * tiles < sms ? (int)(items * tiles) : sms;
+    if (a.grid < 1) a.grid = 1;
+    a.cuts_bytes = ((size_t)sms * sizeof(Cut) + 255) / 256 * 256;
+    a.bytes = a.cuts_bytes + (size_t)sms * 2 * part_floats(a.part_rows, D) * sizeof(float);
+    return a;
 }
 
 }  // namespace
@@ -638,16 +862,28 @@ bool encode_cache(CUtensorMap *map, const ssd_kv_cache &c, const void *data, int
     return encode_map(map, c.dtype, data, 4, dims, strides, b);
 }
 
+size_t tree_attention_workspace_bytes(int Hq, int Hkv, int D, int64_t M, int max_nodes) {
+    int sms = device_sm_count();
+    if (sms <= 0) sms = 148;                          // without a device: the part that the kernels are made for
+    return attention_plan(Hq, Hkv, D, M, max_nodes, 1, 0, sms).bytes;
+}
+
 int launch_tree_attention(const ssd_heads &q, const ssd_heads &tree_k, const ssd_heads &tree_v, const ssd_kv_cache &cache,
                           const int64_t *tok_off, const int32_t *parent, int B, int64_t M, int max_nodes, float scale,
-                          float cap, const ssd_heads &out, float *lse, uint32_t *status, cudaStream_t stream) {
+                          float cap, const ssd_heads &out, float *lse, uint32_t *status, void *workspace, cudaStream_t stream) {
     if (B == 0) return SSD_OK;
+    const int sms = device_sm_count();
+    if (sms <= 0) return SSD_ERR_CUDA;
     AttnParams p;
     p.paging = paging(cache.page_size);
     p.G = q.heads / cache.heads;
-    p.npt = kTile / p.G;
-    if (p.npt > max_nodes) p.npt = max_nodes > 0 ? max_nodes : 1;      // no more of q is fetched than a tree can have
     const int D = cache.head_dim;
+    p.max_pages = cache.pages > 0 ? cache.max_pages : 0;      // without pages every cache is empty
+    const AttnPlan plan = attention_plan(q.heads, cache.heads, D, M, max_nodes, B, (int64_t)p.max_pages * cache.page_size, sms);
+    p.npt = plan.npt;
+    p.part_rows = plan.part_rows;
+    p.cuts = static_cast<Cut *>(workspace);
+    p.parts = reinterpret_cast<float *>(static_cast<char *>(workspace) + plan.cuts_bytes);
     if (M > 0) {
         if (!encode_rows(&p.q, cache.dtype, q, D, M, p.G, p.npt) || !encode_rows(&p.tree_k, cache.dtype, tree_k, D, M, 1, kTreeBox) ||
             !encode_rows(&p.tree_v, cache.dtype, tree_v, D, M, 1, kTreeBox))
@@ -660,19 +896,10 @@ int launch_tree_attention(const ssd_heads &q, const ssd_heads &tree_k, const ssd
     p.out = out.data; p.out_row = out.row_stride; p.out_head = out.head_stride;
     p.lse = lse; p.status = status; p.table_stride = cache.table_stride; p.M = M;
     p.B = B; p.Hq = q.heads; p.Hkv = cache.heads;
-    p.q_items = max_nodes > p.npt ? (max_nodes + 2 * p.npt - 1) / (2 * p.npt) : 1;
     p.max_nodes = max_nodes; p.n_pages = cache.pages;
-    p.max_pages = cache.pages > 0 ? cache.max_pages : 0;      // without pages every cache is empty
     p.scale = scale; p.cap = cap;
-    const int sms = device_sm_count();
-    if (sms <= 0) return SSD_ERR_CUDA;
-    const int64_t items = (int64_t)B * p.Hkv * p.q_items;
-    const int64_t tiles = 1 + ((int64_t)p.max_pages * cache.page_size + kTile - 1) / kTile;
-    p.split = 1;
-    while (p.split < kMaxSplit && items * p.split * 2 <= sms && p.split * 2 <= tiles) p.split *= 2;
-    const int64_t grid = items * p.split;
-    if (grid > INT32_MAX) return SSD_ERR_ARG;
     const bool half = cache.dtype == SSD_F16;
+    const int grid = plan.grid;
     if (D == 64)
         return half ? (cap > 0.f ? launch<__half, 64, true>(p, grid, stream) : launch<__half, 64, false>(p, grid, stream))
                     : (cap > 0.f ? launch<__nv_bfloat16, 64, true>(p, grid, stream) : launch<__nv_bfloat16, 64, false>(p, grid, stream));

@@ -131,8 +131,8 @@ def test_strided_and_partial_inputs(cuda_device):
     both[:, 0], both[:, 1] = d["k"], d["v"]
     d.update(k=both[:, 0], v=both[:, 1])
     wide = torch.full((c.M, 10, 72), 7.0, dtype=c.dtype, device=cuda_device)
-    out = dict(out=wide[:, 1:9, :64], lse=torch.empty(c.M, 8, device=cuda_device),
-               utt_status=torch.empty(2, dtype=torch.int32, device=cuda_device))
+    out = ssd.alloc_tree_attention_outputs(c.M, 2, 8, 64, c.dtype, cuda_device)
+    out["out"] = wide[:, 1:9, :64]
     r = run(c, cuda_device, d=d, out=out)
     check(c, r)
     assert (wide[:, 0] == 7).all() and (wide[:, 9] == 7).all() and (wide[:, :, 64:] == 7).all()

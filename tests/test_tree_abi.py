@@ -33,11 +33,13 @@ P = C.c_void_p
 ref = ssd._ref
 
 
-def attention(lib, q=None, tk=None, tv=None, c=None, off=8, B=2, M=5, max_nodes=4, scale=0.1, cap=0.0, out=None, status=8):
+def attention(lib, q=None, tk=None, tv=None, c=None, off=8, B=2, M=5, max_nodes=4, scale=0.1, cap=0.0, out=None, status=8,
+              ws=256, ws_bytes=1 << 30):
     kv = lambda x: ref(heads(n=2, row=128) if x is None else x)  # noqa: E731
     return lib.ssd_tree_attention(ref(heads() if q is None else q), kv(tk), kv(tv), ref(cache() if c is None else c),
                                   P(off) if off else None, None, B, M, max_nodes, scale, cap,
-                                  ref(heads() if out is None else out), None, P(status) if status else None, None)
+                                  ref(heads() if out is None else out), None, P(status) if status else None, P(ws) if ws else None,
+                                  ws_bytes, None)
 
 
 BAD_CACHES = [(dict(dtype=ssd.F32), ssd.ERR_DTYPE), (dict(dtype=9), ssd.ERR_DTYPE), (dict(page_size=0), ssd.ERR_ARG),
@@ -65,6 +67,11 @@ def test_attention_refuses_bad_arguments(lib):
         assert attention(lib, **kw) == ssd.ERR_ARG, kw
     for kw in (dict(q=heads(data=264)), dict(q=heads(row=516)), dict(tk=heads(n=2, head=68)), dict(out=heads(data=258))):
         assert attention(lib, **kw) == ssd.ERR_ALIGN, kw
+    need = lib.ssd_tree_attention_workspace_bytes(8, 2, 64, 5, 4)
+    assert 0 < need < lib.ssd_tree_attention_workspace_bytes(8, 2, 64, 500, 400) < 1 << 30
+    for kw in (dict(ws=0), dict(ws=264), dict(ws_bytes=need - 1)):
+        assert attention(lib, **kw) == ssd.ERR_WORKSPACE, kw
+    assert lib.ssd_tree_attention_workspace_bytes(8, 3, 64, 5, 4) == 0
 
 
 def append(lib, tk=None, c=None, off=8, path=8, path_len=512, B=2, M=5, weight=8, stride=50, cols=50, new_len=1024, status=8):
