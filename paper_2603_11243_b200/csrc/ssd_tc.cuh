@@ -165,10 +165,12 @@ template <int N> __device__ __forceinline__ void cap_scores(float *x, float scal
     const float r = scale / cap, r2 = r * r;
     const float c1 = -0.33333069394019127f * r2, c2 = 0.13324779317551644f * r2 * r2, c3 = -0.05298607528769192f * r2 * r2 * r2,
                 c4 = 0.01713500662684319f * (r2 * r2) * (r2 * r2);
-    float most = 0.f;
+    float top[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < N; ++i) most = fmax_nan(most, fabsf(x[i]));
-    const bool all_small = __all_sync(0xffffffffu, most * r <= 0.5f);
+    for (int i = 0; i < N; i += 8)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) top[k] = fmaxf(fmaxf(top[k], fabsf(x[i + k])), fabsf(x[i + 4 + k]));      // NaN stays NaN either way
+    const bool all_small = __all_sync(0xffffffffu, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * r <= 0.5f);
     auto poly = [&](float2 v) {
         const float2 t = fmul2(v, v);
         float2 q = ffma2(make_float2(c4, c4), t, make_float2(c3, c3));

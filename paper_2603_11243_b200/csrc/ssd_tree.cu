@@ -72,13 +72,16 @@ template <int D> struct Shape {
     static constexpr int kMl = (kWords + 16 + 15) / 16 * 16;      // [2][128] running maximum and sum
     static constexpr int kParent = kMl + 2 * kTile * 8;
     static constexpr int kSegments = (kParent + kParents * 2 + 15) / 16 * 16;
-    static constexpr int kBytes = kSegments + 2 * 64;
+    static constexpr int kGroups = kSegments + 2 * 64;            // groups of 16 keys in a slot
+    static constexpr int kBytes = kGroups + kSlots * 4;
     static constexpr int kO = 256;                                // tensor memory: scores at 0 and 128, sums here
 };
 static_assert(Shape<128>::kBytes <= 232448, "shared memory");
 
 // ---- the line of key tiles and its cuts -----------------------------------------------------------
-// A tile costs as much as it has tiles of queries, an item 1 more for its end.
+// A tile costs as much as it has tiles of queries, 2,400 clocks each; an item's end costs 6,000 to 8,000 (its last products
+// are waited for, its results written).
+constexpr int kEndCost = 3;
 struct Utterance {
     int64_t i0;
     int n, len, cache_tiles, q_items;
@@ -111,7 +114,7 @@ __device__ __forceinline__ Item item_of(const AttnParams &p, const Utterance &u,
     it.tiles = it.tree_tiles + u.cache_tiles;
     return it;
 }
-__device__ __forceinline__ int64_t cost(const Item &it) { return (int64_t)it.tiles * (1 + it.pair) + 1; }
+__device__ __forceinline__ int64_t cost(const Item &it) { return (int64_t)it.tiles * (1 + it.pair) + kEndCost; }
 __device__ __forceinline__ int64_t cost(const AttnParams &p, const Utterance &u) {     // of one head
     int64_t c = 0;
     for (int qi = 0; qi < u.q_items; ++qi) c += cost(item_of(p, u, qi));
@@ -137,10 +140,9 @@ struct Walk {
     int b, h, qi, begin, end;
     __device__ __forceinline__ bool cut_item(const AttnParams &p) {
         it = item_of(p, u, qi);
-        const int w = 1 + it.pair;
-        const int64_t from = lo - at, to = hi - at;      // tile k lies at at + k w
-        begin = from <= 0 ? 0 : (int)min((from + w - 1) / w, (int64_t)it.tiles);
-        end = to <= 0 ? 0 : (int)min((to + w - 1) / w, (int64_t)it.tiles);
+        const int64_t from = lo - at, to = hi - at;      // tile k lies at at + k (1 + pair)
+        begin = from <= 0 ? 0 : (int)min((from + it.pair) >> it.pair, (int64_t)it.tiles);
+        end = to <= 0 ? 0 : (int)min((to + it.pair) >> it.pair, (int64_t)it.tiles);
         return begin < end;
     }
     __device__ __forceinline__ bool next(const AttnParams &p) {
@@ -160,20 +162,25 @@ struct Walk {
         } while (!cut_item(p));
         return true;
     }
+    // a b / c, in 32 bits where they are enough (they nearly always are, and a division of 64 is a hundred instructions)
+    static __device__ __forceinline__ int64_t scaled(int64_t a, int b, int c) {
+        return a < (1 << 20) ? (int64_t)((uint32_t)a * (uint32_t)b / (uint32_t)c) : a * b / c;      // b is below 2^12: a grid
+    }
     // By one warp: costs[b] are the utterances' (of one head), the first `held` of them.
     __device__ __forceinline__ bool first(const AttnParams &p, const int64_t *costs, int held, int lane) {
         auto head_cost = [&](int i) { return i >= p.B ? 0 : i < held ? costs[i] : cost(p, utterance(p, i)); };
-        int64_t total = 0;
-        for (int i = lane; i < p.B; i += 32) total += head_cost(i);
+        const int64_t mine = head_cost(lane);
+        int64_t total = mine;
+        for (int i = lane + 32; i < p.B; i += 32) total += head_cost(i);
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
         total *= p.Hkv;
-        lo = total * blockIdx.x / gridDim.x;
-        hi = total * (blockIdx.x + 1) / gridDim.x;
+        lo = scaled(total, blockIdx.x, gridDim.x);
+        hi = scaled(total, blockIdx.x + 1, gridDim.x);
         if (lo >= hi) return false;
         int64_t before = 0;
         for (int i0 = 0; i0 < p.B; i0 += 32) {
-            const int64_t one = head_cost(i0 + lane), v = one * p.Hkv;
+            const int64_t one = i0 ? head_cost(i0 + lane) : mine, v = one * p.Hkv;
             int64_t x = v;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
@@ -184,10 +191,11 @@ struct Walk {
             if (here) {
                 const int who = __ffs(here) - 1;         // lo lies in utterance i0 + who
                 b = i0 + who;
+                u = utterance(p, b);
                 const int64_t each = __shfl_sync(0xffffffffu, one, who);
                 at = before + __shfl_sync(0xffffffffu, x - v, who);
-                u = utterance(p, b);
-                h = (int)((lo - at) / each);
+                const int64_t in = lo - at;
+                h = in < (1ll << 31) && each < (1ll << 31) ? (int)((uint32_t)in / (uint32_t)each) : (int)(in / each);
                 at += h * each;
                 for (qi = 0; qi + 1 < u.q_items; ++qi) {
                     const int64_t c = cost(item_of(p, u, qi));
@@ -236,36 +244,69 @@ __device__ __forceinline__ int up_from(const AttnParams &p, int64_t i0, const in
     return up < -1 || up >= j ? -1 : up;
 }
 
-__device__ __forceinline__ bool not_finite16(uint32_t half_bits, uint32_t exponent) { return (half_bits & exponent) == exponent; }
-
 // The product runs over whole groups of 16 keys, and 0 times NaN is NaN: values behind the last key
 // are made zeros, and so are the tree's own values that are not finite (a node that does not see them
 // must not get them; `seen` says that there are some, and those that do see them get them at the end).
-template <typename T>
-__device__ __forceinline__ void clean_values(uint32_t tile, int row, int valid, bool tree, int units, volatile uint32_t *seen) {
+template <typename T, int D>
+__device__ __forceinline__ void clean_values(uint32_t tile, int row, int valid, bool tree, volatile uint32_t *seen) {
     if (row >= valid) {
         if (row < (valid + 15) / 16 * 16)
-            for (int u = 0; u < units; ++u)
+#pragma unroll
+            for (int u = 0; u < D / 8; ++u)
                 asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(unit_at(tile, row, u)), "r"(0) : "memory");
         return;
     }
     if (!tree) return;
-    constexpr uint32_t e = Format<T>::kExponent;
-    for (int u = 0; u < units; ++u) {
+    constexpr uint32_t e = Format<T>::kExponent * 0x10001u;
+    uint32_t bad = 0;                        // a bit for every 4 units that hold something with all exponent bits set
+#pragma unroll
+    for (int u0 = 0; u0 < D / 8; u0 += 4) {
+        uint32_t w[16], hit = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[4 * i]), "=r"(w[4 * i + 1]), "=r"(w[4 * i + 2]), "=r"(w[4 * i + 3])
+                         : "r"(unit_at(tile, row, u0 + i)));
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const uint32_t t = ~w[i] & e;    // a half of zeros: all exponent bits set
+            hit |= (t - 0x00010001u) & ~t & 0x80008000u;
+        }
+        if (hit) bad |= 1u << (u0 / 4);
+    }
+    if (bad == 0) return;
+    *seen = 1;
+    __threadfence_block();
+    for (int u = 0; u < D / 8; ++u) {
+        if (!(bad >> (u / 4) & 1)) continue;
         uint32_t w[4];
         const uint32_t at = unit_at(tile, row, u);
         asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at) : "memory");
-        bool any = false;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const bool lo = not_finite16(w[i], e), hi = not_finite16(w[i] >> 16, e);
-            any |= lo || hi;
-            w[i] &= (lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u);
+            const uint32_t t = ~w[i] & e;
+            w[i] &= (t & 0xffffu ? 0xffffu : 0u) | (t >> 16 ? 0xffff0000u : 0u);
         }
-        if (any) {
-            *seen = 1;
-            __threadfence_block();
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+    }
+}
+
+// N lanes' rows of N 16-byte units each, turned so that a store of the warp writes N units of a row side by side:
+// before, lane i has unit j of row i in v[j]; after, unit i of row j (of its group of N lanes).
+template <int N> __device__ __forceinline__ void turn(uint4 *v) {
+    const int lane = threadIdx.x & (N - 1);
+#pragma unroll
+    for (int o = 1; o < N; o <<= 1) {
+        const bool up = lane & o;
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            if (j & o) continue;
+            // lanes without the bit give v[j | o] and take the partner's v[j], and the other way round
+            uint4 a = up ? v[j] : v[j | o];
+            a.x = __shfl_xor_sync(0xffffffffu, a.x, o);
+            a.y = __shfl_xor_sync(0xffffffffu, a.y, o);
+            a.z = __shfl_xor_sync(0xffffffffu, a.z, o);
+            a.w = __shfl_xor_sync(0xffffffffu, a.w, o);
+            if (up) v[j] = a; else v[j | o] = a;
         }
     }
 }
@@ -300,6 +341,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
     volatile uint32_t *const failed = words + 1;
     float2 *const ml = reinterpret_cast<float2 *>(base + S::kMl);
     int16_t *const parents = reinterpret_cast<int16_t *>(base + S::kParent);
+    volatile int *const groups_of = reinterpret_cast<volatile int *>(base + S::kGroups);
     auto slot_at = [&](int pos) { return smem + S::kRing + (pos % S::kSlots) * S::kSlotBytes; };
 
     if (warp == 8) tmem_alloc(smem + S::kWords, 512);
@@ -386,7 +428,10 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
                     if (pos >= S::kSlots) ok = mbar_wait_bounded(slot_empty(pos), (pos / S::kSlots - 1) & 1);
                     if (!ok) break;
                     const uint32_t bar = slot_full(pos);
-                    if (lane == 0) mbar_arrive_expect_tx(bar, copies * box * 128 * S::kBlocks);
+                    if (lane == 0) {
+                        groups_of[pos % S::kSlots] = (valid + 15) >> 4;
+                        mbar_arrive_expect_tx(bar, copies * box * 128 * S::kBlocks);
+                    }
                     // copies are of 64 columns and 8 rows at least, so 32 lanes are enough
                     const int i = lane / S::kBlocks, x = lane % S::kBlocks;
                     const int page = __shfl_sync(0xffffffffu, id, p.paging.pages ? i : 0);
@@ -406,18 +451,18 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
             int pos0 = 0, used[2] = {0, 0}, buffer = 0, done[2] = {0, 0};
             for (int g = 0; take(g, ok); give(g++)) {
                 const volatile Segment &w = ring[g & 1];
-                const int begin = uniform(w.begin), pair = uniform(w.pair), tiles = uniform(w.end) - begin;
+                const int pair = uniform(w.pair), tiles = uniform(w.end - w.begin);
                 const int units = pair ? 2 * tiles : tiles;
                 for (int i = 0; i < 1 + pair && ok; ++i) {
                     const int q = pair ? i : buffer;
                     ok = mbar_wait_bounded(q_full(q), used[q]++ & 1);
                 }
                 // (stream, tile) pairs in the order of their products: u is of stream u & 1
-                auto groups = [&](int tile) { return uniform((tile_valid(p, w, begin + tile) + 15) >> 4); };     // of 16 keys
-                auto scores = [&](int u, int n16) {
+                auto scores = [&](int u) {                                                // the groups of 16 keys it covers
                     const int s = u & 1, tile = pair ? u >> 1 : u, pos = pos0 + 2 * tile, q = pair ? s : buffer;
                     ok = ok && mbar_wait_bounded(slot_full(pos), (pos / S::kSlots) & 1);
-                    if (!ok) return;
+                    if (!ok) return 0;
+                    const int n16 = uniform(groups_of[pos % S::kSlots]);
                     tc_fence_after();
                     if (elect_one()) {
                         const uint32_t idesc = instruction<T>(n16 * 16, false);
@@ -432,6 +477,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
                         if (tile == tiles - 1) mma_commit(q_empty(q));
                     }
                     __syncwarp();
+                    return n16;
                 };
                 auto values = [&](int u, int n16) {
                     const int s = u & 1, k = u >> 1, tile = pair ? k : u, pos = pos0 + 2 * tile + 1;
@@ -452,16 +498,11 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
                     }
                     __syncwarp();
                 };
-                // what a unit's products need is worked out before its wait
-                int n0 = groups(0), n1 = units > 1 ? groups(pair ? 0 : 1) : 0;
-                if (ok) scores(0, n0);
-                if (units > 1) scores(1, n1);
+                int n0 = ok ? scores(0) : 0, n1 = units > 1 ? scores(1) : 0;
                 for (int u = 0; u < units && ok; ++u) {
-                    const int n2 = u + 2 < units ? groups(pair ? (u + 2) >> 1 : u + 2) : 0;
                     values(u, n0);
-                    if (n2) scores(u + 2, n2);
                     n0 = n1;
-                    n1 = n2;
+                    if (u + 2 < units) n1 = scores(u + 2);
                 }
                 done[0] += (units + 1) >> 1;
                 done[1] += units >> 1;
@@ -544,13 +585,6 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
             const int tile = pair ? k : 2 * k + s, t = begin + tile;
             const bool tree = t < w.tree_tiles;
             const int valid = tile_valid(p, w, t);
-            if (tree || (valid & 15)) {
-                const int pos = pos0 + 2 * tile + 1;
-                ok = ok && mbar_wait_bounded(slot_full(pos), (pos / S::kSlots) & 1);
-                if (!ok) break;
-                clean_values<T>(slot_at(pos), row, valid, tree, D / 8, seen);
-                fence_proxy_async();
-            }
             ok = mbar_wait_bounded(scores_full(s), (done + k) & 1);
             if (!ok) break;
             tc_fence_after();
@@ -592,7 +626,11 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
                         }
                     }
 #pragma unroll
-                    for (int i = 0; i < kTile; ++i) x[i] = see[i >> 5] >> (i & 31) & 1 ? x[i] : -INFINITY;
+                    for (int j = 0; j < 4; ++j) {
+                        if (__all_sync(0xffffffffu, see[j] == 0xffffffffu)) continue;
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) x[j * 32 + i] = see[j] >> i & 1 ? x[j * 32 + i] : -INFINITY;
+                    }
                 }
                 float top[4] = {x[0], x[1], x[2], x[3]};
 #pragma unroll
@@ -608,7 +646,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
                     const float f = old == -INFINITY ? 0.f : ex2((old - m) * c);
                     l *= f;
                     if (k > 0) {
-#pragma unroll
+#pragma unroll 1
                         for (int j = 0; j < D / 16; ++j) {       // a few at a time: the scores fill the registers
                             float o[16];
                             tmem_ld16(t_sums + j * 16, o);
@@ -640,6 +678,13 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
                 l += sum[0].x + sum[0].y;
                 tmem_wait_st();
             }
+            if (tree || (valid & 15)) {              // by now the values are there
+                const int pos = pos0 + 2 * tile + 1;
+                ok = mbar_wait_bounded(slot_full(pos), (pos / S::kSlots) & 1);
+                if (!ok) break;
+                clean_values<T, D>(slot_at(pos), row, valid, tree, seen);
+                fence_proxy_async();
+            }
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(probs_ready(s));
@@ -669,49 +714,57 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
         }
         const bool whole = begin == 0 && w.end == w.tiles;
         float *const part = p.parts + (2 * (int64_t)blockIdx.x + (begin == 0)) * part_floats(p.part_rows, D);
-        const int64_t out_at = (w.i0 + node) * p.out_row + head * p.out_head;
         const float inv = !whole ? 1.f : l == 0.f ? 0.f : 1.f / l;
-        const uint32_t own = tmem + S::kO + lanes;
-        constexpr int kChunks = D / 32;
-        const int j0 = pair ? 0 : s * (kChunks / 2), j1 = pair ? kChunks : j0 + kChunks / 2;
+        w0 *= inv;
+        w1 *= inv;
+        const int64_t i0 = w.i0, out_at = (i0 + node) * p.out_row + head * p.out_head;
+        const int j0 = pair ? 0 : s * (D / 2), j1 = pair ? D : j0 + D / 2;
         if (busy) {
-            for (int j = j0; j < j1; ++j) {
+            // 32 columns at a time and the loop not unrolled: straight code that runs once an item waits for its
+            // instructions (9,400 clocks an item unrolled)
+#pragma unroll 1
+            for (int j = j0; j < j1; j += 32) {
                 float o[32];
-                tmem_ld32(own + (pair ? s * D : 0) + j * 32, o);
+                tmem_ld32(tmem + S::kO + lanes + (pair ? s * D : 0) + j, o);
                 tmem_wait_ld();
 #pragma unroll
-                for (int i = 0; i < 32; ++i) o[i] = o[i] * w0 * inv;
+                for (int i = 0; i < 32; ++i) o[i] *= w0;
                 if (!pair && any[1]) {
                     float o1[32];
-                    tmem_ld32(own + D + j * 32, o1);
+                    tmem_ld32(tmem + S::kO + lanes + D + j, o1);
                     tmem_wait_ld();
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) o[i] = fmaf(o1[i], w1 * inv, o[i]);
+                    for (int i = 0; i < 32; ++i) o[i] = fmaf(o1[i], w1, o[i]);
                 }
                 if (sick && live) {
                     // values that are not finite, to the nodes that see them
-                    for (int a = node; a >= 0; a = up_from(p, w.i0, parents, a)) {
-                        const T *v = reinterpret_cast<const T *>(p.tree_v_at) + (w.i0 + a) * p.tree_row + w.h * p.tree_head + j * 32;
+                    for (int a = node; a >= 0; a = up_from(p, i0, parents, a)) {
+                        const T *y = reinterpret_cast<const T *>(p.tree_v_at) + (i0 + a) * p.tree_row + w.h * p.tree_head + j;
 #pragma unroll
                         for (int i = 0; i < 32; ++i) {
-                            const float y = (float)v[i];
-                            if (!(fabsf(y) < INFINITY)) o[i] += y;
+                            const float z = (float)y[i];
+                            if (!(fabsf(z) < INFINITY)) o[i] += z;
                         }
                     }
                 }
-                if (live) {
-                    if (whole) {
-                        T *const to = reinterpret_cast<T *>(p.out) + out_at + j * 32;
+                if (whole) {
+                    uint4 v[4];
 #pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            reinterpret_cast<uint4 *>(to)[i] =
-                                make_uint4(pack2<T>(o[8 * i], o[8 * i + 1]), pack2<T>(o[8 * i + 2], o[8 * i + 3]),
-                                           pack2<T>(o[8 * i + 4], o[8 * i + 5]), pack2<T>(o[8 * i + 6], o[8 * i + 7]));
-                    } else {
-                        float4 *const to = reinterpret_cast<float4 *>(part + 2 * p.part_rows + (int64_t)(tile_q * tile_rows + row) * D + j * 32);
+                    for (int i = 0; i < 4; ++i)
+                        v[i] = make_uint4(pack2<T>(o[8 * i], o[8 * i + 1]), pack2<T>(o[8 * i + 2], o[8 * i + 3]),
+                                          pack2<T>(o[8 * i + 4], o[8 * i + 5]), pack2<T>(o[8 * i + 6], o[8 * i + 7]));
+                    turn<4>(v);
+                    const int of = lane & ~3;
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) to[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                    for (int k = 0; k < 4; ++k) {
+                        const int64_t at = __shfl_sync(0xffffffffu, out_at, of + k);
+                        if (quad * 32 + of + k < rows)
+                            *reinterpret_cast<uint4 *>(reinterpret_cast<T *>(p.out) + at + j + (lane & 3) * 8) = v[k];
                     }
+                } else if (live) {
+                    float4 *const to = reinterpret_cast<float4 *>(part + 2 * p.part_rows + (int64_t)(tile_q * tile_rows + row) * D + j);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) to[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
                 }
             }
         }
@@ -744,41 +797,53 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
     if (tid == 0) p.cuts[blockIdx.x].failed = *failed != 0;
 }
 
-// Joins the parts of the item that begins in CTA blockIdx.x of the line and goes on behind it; four
-// blocks share its values.
-constexpr int kJoinBlocks = 4, kJoinThreads = 256;
+// Joins the parts of the item that begins in CTA blockIdx.x / kJoinBlocks of the line and goes on behind it: a
+// thread has four columns of a row.
+constexpr int kJoinBlocks = 16, kJoinThreads = 256, kJoinAhead = 4;
 
 template <typename T, int D, bool kCap>
 __global__ void __launch_bounds__(kJoinThreads) tree_attention_join(const __grid_constant__ AttnParams p, int grid) {
     pdl_enter();
-    const int first = blockIdx.x / kJoinBlocks;
+    const int first = blockIdx.x / kJoinBlocks, slice = blockIdx.x % kJoinBlocks;
     const Cut cut = p.cuts[first];
-    if (cut.failed && blockIdx.x % kJoinBlocks == 0)
+    if (cut.failed && slice == 0)
         for (int b = cut.first_b + threadIdx.x; b <= cut.last_b; b += kJoinThreads) p.status[b] = SSD_UTT_INTERNAL;
-    if (!cut.tail) return;
-    int last = first + 1;                            // the CTA that the item ends in
-    while (last < grid && p.cuts[last].head != 2) ++last;
-    if (last == grid) return;
+    if (!cut.tail || slice * kJoinThreads >= cut.rows * (D / 4)) return;
     const float c = kCap ? kLog2e : p.scale * kLog2e;
     const int64_t stride = 2 * part_floats(p.part_rows, D);
-    const float *const tail = p.parts + first * stride + part_floats(p.part_rows, D);
     const int64_t i0 = p.off[cut.b];
-    for (int e = blockIdx.x % kJoinBlocks * kJoinThreads + threadIdx.x; e < cut.rows * (D / 4); e += kJoinBlocks * kJoinThreads) {
+    for (int e = slice * kJoinThreads + threadIdx.x; e < cut.rows * (D / 4); e += kJoinBlocks * kJoinThreads) {
         const int r = e / (D / 4), u = e - r * (D / 4);
         float m = -INFINITY, l = 0.f;
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int k = first; k <= last; ++k) {
-            if (k > first && k < last && p.cuts[k].head == 0) continue;      // too short a part for a tile
-            const float *const part = k == first ? tail : p.parts + k * stride;
-            const float2 a = reinterpret_cast<const float2 *>(part)[r];
-            const float4 v = reinterpret_cast<const float4 *>(part + 2 * p.part_rows + (int64_t)r * D)[u];
-            const float top = fmaxf(m, a.x);
-            const float f = m > -INFINITY ? ex2((m - top) * c) : 0.f, g = a.x > -INFINITY ? ex2((a.x - top) * c) : a.y;
-            // without a score (a.y == 0) nothing is added; with NaN scores alone (a.y is NaN) it is NaN
-            l = fmaf(l, f, a.x > -INFINITY ? g * a.y : a.y);
-            o.x = fmaf(o.x, f, g * v.x); o.y = fmaf(o.y, f, g * v.y);
-            o.z = fmaf(o.z, f, g * v.z); o.w = fmaf(o.w, f, g * v.w);
-            m = top;
+        bool more = true;
+        for (int k0 = first; more && k0 < grid; k0 += kJoinAhead) {
+            // the part of CTA `first` is its second; those behind are the others' first.  A few at a time, fetched
+            // before it is known whether they are there.
+            int head[kJoinAhead];
+            float2 a[kJoinAhead];
+            float4 v[kJoinAhead];
+#pragma unroll
+            for (int i = 0; i < kJoinAhead; ++i) {
+                const int k = k0 + i < grid ? k0 + i : grid - 1;
+                const float *const part = p.parts + k * stride + (k == first ? stride / 2 : 0);
+                head[i] = p.cuts[k].head;
+                a[i] = reinterpret_cast<const float2 *>(part)[r];
+                v[i] = reinterpret_cast<const float4 *>(part + 2 * p.part_rows + (int64_t)r * D)[u];
+            }
+#pragma unroll
+            for (int i = 0; i < kJoinAhead; ++i) {
+                const int k = k0 + i;
+                if (!more || k >= grid || (k > first && head[i] == 0)) continue;      // 0: too short a part for a tile
+                const float top = fmaxf(m, a[i].x);
+                const float f = m > -INFINITY ? ex2((m - top) * c) : 0.f, g = a[i].x > -INFINITY ? ex2((a[i].x - top) * c) : a[i].y;
+                // without a score (the sum is 0) nothing is added; with NaN scores alone (it is NaN) all becomes NaN
+                l = fmaf(l, f, a[i].x > -INFINITY ? g * a[i].y : a[i].y);
+                o.x = fmaf(o.x, f, g * v[i].x); o.y = fmaf(o.y, f, g * v[i].y);
+                o.z = fmaf(o.z, f, g * v[i].z); o.w = fmaf(o.w, f, g * v[i].w);
+                m = top;
+                if (k > first && head[i] == 2) more = false;
+            }
         }
         const float inv = l == 0.f ? 0.f : 1.f / l;
         const int64_t node = i0 + cut.node0 + r / p.G;
