@@ -188,7 +188,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) cache_weights(const __grid_con
                     const bool half = rows - j <= 16;            // the product wrote no more than that
                     if (half) tmem_ld16(t_scores + j, x); else tmem_ld32(t_scores + j, x);
                     tmem_wait_ld();
-                    if (kCap) { if (half) cap_scores<16>(x, p.scale, p.cap); else cap_scores<32>(x, p.scale, p.cap); }
+                    if (kCap) { if (half) cap_scores<16>(x, p.scale, p.cap, row < at.valid); else cap_scores<32>(x, p.scale, p.cap, row < at.valid); }
 #pragma unroll
                     for (int i = 0; i < 32; ++i) {
                         if (i >= 16 && half) break;

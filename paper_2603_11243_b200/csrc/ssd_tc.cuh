@@ -161,7 +161,8 @@ template <> __device__ __forceinline__ uint32_t pack2<__half>(float lo, float hi
 // packed operations for two scores and none on the special-function unit, which the softmax needs.  Where a
 // score of the warp is larger, y >= 1/2 goes through 1 - 2 / (1 + e^2y): its error, 1e-7, is then relative to
 // at least 0.46.
-template <int N> __device__ __forceinline__ void cap_scores(float *x, float scale, float cap) {
+// `counts`: whether the thread's scores are anybody's (what lies in other rows must not send a warp the long way).
+template <int N> __device__ __forceinline__ void cap_scores(float *x, float scale, float cap, bool counts) {
     const float r = scale / cap, r2 = r * r;
     const float c1 = -0.33333069394019127f * r2, c2 = 0.13324779317551644f * r2 * r2, c3 = -0.05298607528769192f * r2 * r2 * r2,
                 c4 = 0.01713500662684319f * (r2 * r2) * (r2 * r2);
@@ -170,7 +171,7 @@ template <int N> __device__ __forceinline__ void cap_scores(float *x, float scal
     for (int i = 0; i < N; i += 8)
 #pragma unroll
         for (int k = 0; k < 4; ++k) top[k] = fmaxf(fmaxf(top[k], fabsf(x[i + k])), fabsf(x[i + 4 + k]));      // NaN stays NaN either way
-    const bool all_small = __all_sync(0xffffffffu, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * r <= 0.5f);
+    const bool all_small = __all_sync(0xffffffffu, !counts || fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * r <= 0.5f);
     auto poly = [&](float2 v) {
         const float2 t = fmul2(v, v);
         float2 q = ffma2(make_float2(c4, c4), t, make_float2(c3, c3));

@@ -239,7 +239,7 @@ __device__ __forceinline__ void report(const AttnParams &p, int b, int lane) {
 
 __device__ __forceinline__ int up_from(const AttnParams &p, int64_t i0, const int16_t *parents, int j) {
     if (!p.parent) return j - 1;
-    if (j < kParents) return parents[j];
+    if (parents && j < kParents) return parents[j];
     const int up = p.parent[i0 + j];
     return up < -1 || up >= j ? -1 : up;
 }
@@ -572,7 +572,24 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
         const int count = pair ? tiles : (tiles - s + 1) >> 1;
         volatile uint32_t *const seen = words + 2 + (g & 1);
 
-        if (p.parent && begin < w.tree_tiles) {
+        // A tree of up to 32 nodes: a lane has a node, and five rounds of doubling over the lanes give its line.  Larger
+        // ones are walked, from parents in shared memory (5,000 clocks an item where this takes 400).
+        const bool small = p.parent && w.last <= 32;
+        uint32_t line = 0;
+        if (small && begin < w.tree_tiles) {
+            int up = lane < w.last ? p.parent[w.i0 + lane] : -1;
+            if (up < -1 || up >= lane) up = -1;
+            uint32_t mask = 1u << lane;
+#pragma unroll
+            for (int round = 0; round < 5; ++round) {
+                const int from = up < 0 ? lane : up;
+                const uint32_t above = __shfl_sync(0xffffffffu, mask, from);
+                const int further = __shfl_sync(0xffffffffu, up, from);
+                if (up >= 0) { mask |= above; up = further; }
+            }
+            line = __shfl_sync(0xffffffffu, mask, node & 31);
+        }
+        if (p.parent && !small && begin < w.tree_tiles) {
             for (int j = tid; j < min(w.last, kParents); j += 256) {
                 const int up = p.parent[w.i0 + j];
                 parents[j] = (int16_t)(up < -1 || up >= j ? -1 : up);
@@ -599,7 +616,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
                     }
                 }
                 tmem_wait_ld();
-                if (kCap) cap_scores<kTile>(x, p.scale, p.cap);
+                if (kCap) cap_scores<kTile>(x, p.scale, p.cap, live);
                 if (tree || valid < kTile) {
                     uint32_t see[4];
 #pragma unroll
@@ -609,7 +626,9 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
                     }
                     if (tree) {
                         const int t0 = tree_tile_start(w, t);
-                        if (!p.parent) {
+                        if (small) {
+                            see[0] = line;
+                        } else if (!p.parent) {
 #pragma unroll
                             for (int j = 0; j < 4; ++j) {
                                 const int left = node + 1 - t0 - j * 32;
@@ -639,7 +658,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
                     for (int k = 0; k < 4; ++k)
                         top[k] = i + 4 + k < kTile ? fmaxf(fmaxf(top[k], x[i + k]), x[i + 4 + k]) : fmaxf(top[k], x[i + k]);
                 const float mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(fmaxf(top[2], top[3]), -INFINITY));
-                const bool grow = mx > m + lag || (m == -INFINITY && mx > m);
+                const bool grow = live && (mx > m + lag || (m == -INFINITY && mx > m));
                 if (__any_sync(0xffffffffu, grow)) {
                     const float old = m;
                     m = fmaxf(m, mx);
@@ -738,7 +757,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
                 }
                 if (sick && live) {
                     // values that are not finite, to the nodes that see them
-                    for (int a = node; a >= 0; a = up_from(p, i0, parents, a)) {
+                    for (int a = node; a >= 0; a = up_from(p, i0, small ? nullptr : parents, a)) {
                         const T *y = reinterpret_cast<const T *>(p.tree_v_at) + (i0 + a) * p.tree_row + w.h * p.tree_head + j;
 #pragma unroll
                         for (int i = 0; i < 32; ++i) {
