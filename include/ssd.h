@@ -411,7 +411,7 @@ int32_t ssd_verify_combine(const float *stats_all, int32_t R, int64_t V_total,
  *
  * Keys, values, queries and attention outputs are SSD_BF16 or SSD_F16, heads are 64 or 128 values
  * long and contiguous; every base address and every stride of an axis with more than one entry is a
- * multiple of 16 bytes (else SSD_ERR_ALIGN).  Strides count elements.
+ * multiple of 16 bytes (else SSD_ERR_ALIGN).  Strides count elements.  A cache has at most 2^31 - 1 slots.
  */
 typedef struct ssd_heads {     /* an array [M, heads, head_dim] */
     void *data;
@@ -525,8 +525,8 @@ int32_t ssd_cache_weights(const ssd_heads *q, const float *lse, const ssd_kv_cac
  *   weight_out[b * weight_out_stride + j] = weight[b * weight_stride + kept]; 0 behind      (nullable)
  * What lies behind new_len in the cache is left as it was.  weight is not changed (weight_out is another
  * array); new_len may be cache->len.  Pages are one utterance's own: one that two share would be
- * compacted twice.  A len out of range is clamped, one above weight_cols (and the budget) to that; entries in
- * bad pages are not moved (SSD_UTT_BAD_CACHE for all three).
+ * compacted twice.  A len out of range is clamped, one above both weight_cols and the budget to the larger of
+ * them; slots in bad pages are not moved (SSD_UTT_BAD_CACHE for all three).
  * kept [B, budget] i32.
  * Errors: SSD_ERR_NULL, SSD_ERR_ARG (also sink + recent > budget), SSD_ERR_DTYPE, SSD_ERR_ALIGN, SSD_ERR_CUDA.
  */

@@ -380,7 +380,7 @@ static int check_cache(const ssd_kv_cache &c, int32_t B, bool values) {
     if (c.dtype != SSD_BF16 && c.dtype != SSD_F16) return SSD_ERR_DTYPE;
     if (c.pages < 0 || c.page_size < 1 || c.heads < 1 || c.max_pages < 0 || (c.head_dim != 64 && c.head_dim != 128))
         return SSD_ERR_ARG;
-    if (c.table_stride < (B > 1 ? c.max_pages : 0)) return SSD_ERR_ARG;
+    if (c.table_stride < (B > 1 ? c.max_pages : 0) || (int64_t)c.pages * c.page_size > INT32_MAX) return SSD_ERR_ARG;
     if (B > 0 && (!c.len || (c.max_pages > 0 && !c.page_table))) return SSD_ERR_NULL;
     if (c.pages > 0 && (!c.k || (values && !c.v))) return SSD_ERR_NULL;
     if (c.page_stride < 0 || c.slot_stride < 0 || c.head_stride < 0) return SSD_ERR_ARG;

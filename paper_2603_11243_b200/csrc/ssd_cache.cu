@@ -49,7 +49,7 @@ struct AppendParams {
     uint32_t *status;
 };
 
-constexpr int kAppendThreads = 256;
+constexpr int kAppendThreads = 256, kAppendRows = 4;
 
 __global__ void __launch_bounds__(kAppendThreads) append_kernel(const AppendParams p) {
     pdl_enter();
@@ -65,17 +65,32 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(const AppendPara
     if (take < 0 || (rows_ok && take > n)) bits |= SSD_UTT_BAD_PARENT;
     if (!bits && len + (int64_t)take > room) bits |= SSD_UTT_CACHE_FULL;
     const int count = bits ? 0 : take;
-    const int per_row = 2 * p.c.heads * p.c.units, step = p.parts * kAppendThreads;
-    const int64_t all = (int64_t)count * per_row;
-    for (int64_t e = (int64_t)part * kAppendThreads + tid; e < all; e += step) {
-        const int k = (int)(e / per_row), r = (int)(e - (int64_t)k * per_row);
-        const int kv = r >= p.c.heads * p.c.units, hu = kv ? r - p.c.heads * p.c.units : r;
-        const int h = hu / p.c.units, u = hu - h * p.c.units;
-        const int j = p.path ? p.path[i0 + k] : k;
-        const int64_t at = slot_at(p.c, b, len + k);
-        if (j < 0 || j >= n || at < 0) continue;
-        const uint4 *from = kv ? p.tree_v + (i0 + j) * p.v_row + h * p.v_head : p.tree_k + (i0 + j) * p.k_row + h * p.k_head;
-        (kv ? p.c.v : p.c.k)[at + h * p.c.head_stride + u] = from[u];
+    // This part's rows of the path.  A thread keeps its place in a row (tree keys or values, head, 16-byte unit) and goes
+    // down the rows four at a time, whose look-ups and loads are then under way together.
+    const int rows = (count + p.parts - 1) / p.parts, k0 = part * rows, k1 = min(count, k0 + rows);
+    const int half = p.c.heads * p.c.units;
+    for (int r = tid; r < 2 * half; r += kAppendThreads) {
+        const int kv = r >= half, hu = kv ? r - half : r, h = hu / p.c.units, u = hu - h * p.c.units;
+        const uint4 *const from = (kv ? p.tree_v + h * p.v_head : p.tree_k + h * p.k_head) + u;
+        const int64_t row_stride = kv ? p.v_row : p.k_row;
+        uint4 *const to = (kv ? p.c.v : p.c.k) + h * p.c.head_stride + u;
+        for (int k = k0; k < k1; k += kAppendRows) {
+            int j[kAppendRows];
+            int64_t at[kAppendRows];
+            uint4 x[kAppendRows];
+#pragma unroll
+            for (int i = 0; i < kAppendRows; ++i) {
+                const int q = min(k + i, k1 - 1);            // the last row again rather than a branch
+                j[i] = p.path ? p.path[i0 + q] : q;
+                at[i] = slot_at(p.c, b, len + q);
+            }
+#pragma unroll
+            for (int i = 0; i < kAppendRows; ++i)
+                if (j[i] >= 0 && j[i] < n && at[i] >= 0) x[i] = from[(i0 + j[i]) * row_stride];
+#pragma unroll
+            for (int i = 0; i < kAppendRows; ++i)
+                if (j[i] >= 0 && j[i] < n && at[i] >= 0 && k + i < k1) to[at[i]] = x[i];
+        }
     }
     if (part == 0) {
         for (int k = tid; k < count; k += kAppendThreads) {
@@ -115,54 +130,143 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
 
 constexpr int kSelectThreads = 1024;
 
-// Exclusive sum of `v` over the block in thread order, and the block's total.
-__device__ __forceinline__ int block_scan(int v, int *warp_sums, int &total) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+// The sum of `v` over a warp's lanes before this one.
+__device__ __forceinline__ int lanes_before(int v) {
+    const int lane = threadIdx.x & 31;
     int x = v;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
         const int y = __shfl_up_sync(0xffffffffu, x, o);
         if (lane >= o) x += y;
     }
-    if (lane == 31) warp_sums[warp] = x;
-    __syncthreads();
-    if (warp == 0) {
-        int s = warp_sums[lane];
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int y = __shfl_up_sync(0xffffffffu, s, o);
-            if (lane >= o) s += y;
-        }
-        warp_sums[lane] = s;
-    }
-    __syncthreads();
-    const int before = warp ? warp_sums[warp - 1] : 0;
-    total = warp_sums[31];
-    __syncthreads();
-    return before + x - v;
+    return x - v;
 }
 
 // One CTA per utterance: the k-th largest key of the slots between the first `sink` and the last `recent`
-// by four rounds of 8 bits, then the kept slots in order (of equal keys the lowest slots).
+// by four rounds of 8 bits, then the kept slots in order (of equal keys the lowest slots).  A warp has a
+// run of consecutive slots, 32 at a time: up to 16,384 slots their keys stay in registers and are fetched once.
+constexpr int kKeys = 16, kSelectWarps = kSelectThreads / 32;
+
+struct SelectShared {
+    int hist[256];
+    int greater[kSelectWarps], equal[kSelectWarps];    // of a warp's slots; then what lies before them
+    int digit, left;
+    unsigned any;
+};
+
+template <bool kHeld>
+__device__ __forceinline__ void select_slots(const EvictParams &p, SelectShared &sh, const float *w, int len, int32_t *kept, float *wout) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int lo = p.sink, hi = len - p.recent, want = p.budget - p.sink - p.recent;
+    const int steps = (len + kSelectThreads - 1) / kSelectThreads, mine = warp * steps * 32 + lane;      // + 32 a step
+    float held[kHeld ? kKeys : 1];
+    if (kHeld) {
+#pragma unroll
+        for (int i = 0; i < kKeys; ++i) held[i] = i < steps && mine + i * 32 < len ? w[mine + i * 32] : 0.f;
+    }
+    auto each = [&](auto body) {                       // body(slot, weight) for all of this thread's, whole warps at a time
+        if (kHeld) {
+#pragma unroll
+            for (int i = 0; i < kKeys; ++i)
+                if (i < steps) body(mine + i * 32, held[i]);
+        } else {
+            for (int i = 0; i < steps; ++i) body(mine + i * 32, mine + i * 32 < len ? w[mine + i * 32] : 0.f);
+        }
+    };
+    uint32_t prefix = 0, mask = 0;
+    int left = want;                                   // to be taken of the keys that match the prefix
+    if (want > 0) {
+        for (int shift = 24; shift >= 0; shift -= 8) {
+            if (tid < 256) sh.hist[tid] = 0;
+            __syncthreads();
+            each([&](int i, float x) {
+                const uint32_t key = weight_key(x);
+                const bool in = i >= lo && i < hi && (key & mask) == prefix;
+                // weights share their leading bits: lanes with the same digit count as one
+                const uint32_t digit = in ? key >> shift & 255 : 256u;
+                const unsigned same = __match_any_sync(0xffffffffu, digit);
+                if (in && (__ffs(same) - 1) == lane) atomicAdd(&sh.hist[digit], __popc(same));
+            });
+            __syncthreads();
+            if (tid < 32) {                            // the digit at which the count from above reaches `left`
+                int sum = 0;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum += sh.hist[255 - (tid * 8 + i)];
+                int above = lanes_before(sum);
+                if (above < left && above + sum >= left) {
+                    for (int i = 0; i < 8; ++i) {
+                        const int d = 255 - (tid * 8 + i), c = sh.hist[d];
+                        if (above + c >= left) { sh.digit = d; sh.left = left - above; break; }
+                        above += c;
+                    }
+                }
+            }
+            __syncthreads();
+            left = sh.left;
+            prefix |= (uint32_t)sh.digit << shift;
+            mask |= 255u << shift;
+        }
+    }
+    // what a warp takes for certain (the ends, and larger keys) and what it has of the last key
+    int sure = 0, equals = 0;
+    auto kind = [&](int i, float x, bool &certain, bool &equal) {
+        const uint32_t key = weight_key(x);
+        const bool middle = i >= lo && i < hi && want > 0;
+        certain = i < lo || (i >= hi && i < len) || (middle && key > prefix);
+        equal = middle && key == prefix;
+    };
+    each([&](int i, float x) {
+        bool certain, equal;
+        kind(i, x, certain, equal);
+        sure += __popc(__ballot_sync(0xffffffffu, certain));
+        equals += __popc(__ballot_sync(0xffffffffu, equal));
+    });
+    if (lane == 0) { sh.greater[warp] = sure; sh.equal[warp] = equals; }
+    __syncthreads();
+    if (warp == 0) {
+        const int g = sh.greater[lane], e = sh.equal[lane];
+        const int e_before = lanes_before(e);
+        const int taken = min(e, max(left - e_before, 0));
+        const int at = lanes_before(g + taken);
+        sh.greater[lane] = at;
+        sh.equal[lane] = e_before;
+    }
+    __syncthreads();
+    int at = sh.greater[warp], equal_before = sh.equal[warp];
+    const unsigned below = (1u << lane) - 1;
+    each([&](int i, float x) {
+        bool certain, equal;
+        kind(i, x, certain, equal);
+        const unsigned eq = __ballot_sync(0xffffffffu, equal);
+        const bool take = certain || (equal && equal_before + __popc(eq & below) < left);
+        const unsigned all = __ballot_sync(0xffffffffu, take);
+        if (take) {
+            const int to = at + __popc(all & below);
+            kept[to] = i;
+            if (wout) wout[to] = x;
+        }
+        at += __popc(all);
+        equal_before += __popc(eq);
+    });
+}
+
 __global__ void __launch_bounds__(kSelectThreads) select_kernel(const EvictParams p) {
-    __shared__ int hist[256], warp_sums[32];
-    __shared__ int s_digit, s_left;
-    __shared__ unsigned any;
+    __shared__ SelectShared sh;
     pdl_enter();
     const int b = blockIdx.x, tid = threadIdx.x;
     const int64_t room = room_of(p.c);
     const int given = p.c.len[b];
     int len = min(max(given, 0), (int)room);
     uint32_t bits = given == len ? 0u : SSD_UTT_BAD_CACHE;
-    if (len > p.budget && len > p.weight_cols) { bits |= SSD_UTT_BAD_CACHE; len = p.weight_cols; }
-    if (tid == 0) any = 0;
+    if (len > p.budget && len > p.weight_cols) { bits |= SSD_UTT_BAD_CACHE; len = max(p.budget, p.weight_cols); }
+    if (tid == 0) sh.any = 0;
     __syncthreads();
     const int pages = (int)(((int64_t)len + p.c.page - 1) / p.c.page);
     for (int j = tid; j < pages; j += kSelectThreads) {
         const int id = p.c.table[b * p.c.table_stride + j];
         if (id < 0 || id >= p.c.pages) bits |= SSD_UTT_BAD_CACHE;
     }
-    if (bits) atomicOr(&any, bits);
+    if (bits) atomicOr(&sh.any, bits);
     const float *const w = p.weight + b * p.weight_stride;
     int32_t *const kept = p.kept + (int64_t)b * p.budget;
     float *const wout = p.weight_out ? p.weight_out + b * p.out_stride : nullptr;
@@ -176,102 +280,69 @@ __global__ void __launch_bounds__(kSelectThreads) select_kernel(const EvictParam
             kept[j] = j;
             if (wout) wout[j] = j < p.weight_cols ? w[j] : 0.f;
         }
+    } else if (len <= kKeys * kSelectThreads) {
+        select_slots<true>(p, sh, w, len, kept, wout);
     } else {
-        const int lo = p.sink, hi = len - p.recent, want = p.budget - p.sink - p.recent;
-        uint32_t prefix = 0, mask = 0;
-        int left = want;                               // to be taken of the keys that match the prefix
-        if (want > 0) {
-            for (int shift = 24; shift >= 0; shift -= 8) {
-                for (int i = tid; i < 256; i += kSelectThreads) hist[i] = 0;
-                __syncthreads();
-                for (int i = lo + tid; i < hi; i += kSelectThreads) {
-                    const uint32_t key = weight_key(w[i]);
-                    if ((key & mask) == prefix) atomicAdd(&hist[key >> shift & 255], 1);
-                }
-                __syncthreads();
-                if (tid < 32) {                        // the digit at which the count from above reaches `left`
-                    int sum = 0;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) sum += hist[255 - (tid * 8 + i)];
-                    int x = sum;
-#pragma unroll
-                    for (int o = 1; o < 32; o <<= 1) {
-                        const int y = __shfl_up_sync(0xffffffffu, x, o);
-                        if (tid >= o) x += y;
-                    }
-                    int above = x - sum;
-                    if (above < left && x >= left) {
-                        for (int i = 0; i < 8; ++i) {
-                            const int d = 255 - (tid * 8 + i), c = hist[d];
-                            if (above + c >= left) { s_digit = d; s_left = left - above; break; }
-                            above += c;
-                        }
-                    }
-                }
-                __syncthreads();
-                left = s_left;
-                prefix |= (uint32_t)s_digit << shift;
-                mask |= 255u << shift;
-                __syncthreads();
-            }
-        }
-        int at = 0, equal_before = 0;
-        for (int base = 0; base < len; base += kSelectThreads) {
-            const int i = base + tid;
-            const float x = i < len ? w[i] : 0.f;
-            const uint32_t key = weight_key(x);
-            const bool forced = i < lo || (i >= hi && i < len), middle = i >= lo && i < hi && want > 0;
-            const bool equal = middle && key == prefix;
-            int equals, total;
-            const int rank = block_scan(equal, warp_sums, equals);
-            const bool take = forced || (middle && key > prefix) || (equal && equal_before + rank < left);
-            const int to = at + block_scan(take, warp_sums, total);
-            if (take) {
-                kept[to] = i;
-                if (wout) wout[to] = x;
-            }
-            at += total;
-            equal_before += equals;
-        }
+        select_slots<false>(p, sh, w, len, kept, wout);
     }
     __syncthreads();
-    if (tid == 0) { p.new_len[b] = count; p.status[b] = any; }
+    if (tid == 0) { p.new_len[b] = count; p.status[b] = sh.any; }
 }
 
 // Kept slots move down in order, kept[j] to j.  kept[j] >= j, and ascending, so a block of slots may be
 // written once all of its own sources have been read: later blocks' sources lie behind it.
-constexpr int kMoveThreads = 512, kMoveRows = 8;
+// Where slots lie is looked up for a thousand rows ahead, so that a block of rows costs one round trip.
+constexpr int kMoveThreads = 256, kMoveRows = 8, kMoveAhead = 1024;
 
 __global__ void __launch_bounds__(kMoveThreads) move_kernel(const EvictParams p) {
+    // slot numbers over all pages (page id times page size and the slot in it), or -1
+    __shared__ int from[kMoveAhead], to[kMoveAhead];
     pdl_enter();
     const int kv = blockIdx.x & 1, h = blockIdx.x / 2 % p.c.heads, b = blockIdx.x / 2 / p.c.heads, tid = threadIdx.x;
     const int count = p.new_len[b];
     const int32_t *const kept = p.kept + (int64_t)b * p.budget;
-    uint4 *const base = (kv ? p.c.v : p.c.k) + h * p.c.head_stride;
+    const int32_t *const table = p.c.table + b * p.c.table_stride;
     const int u = tid % p.c.units, r0 = tid / p.c.units, rows = kMoveThreads / p.c.units;
+    uint4 *const base = (kv ? p.c.v : p.c.k) + h * p.c.head_stride + u;
     // slots before the first gap stay: kept[j] == j holds up to there and nowhere behind
+    if (count == 0 || kept[count - 1] == count - 1) return;
     int first = 0, end = count;
     while (first < end) {
         const int mid = (first + end) >> 1;
         if (kept[mid] == mid) first = mid + 1; else end = mid;
     }
-    for (int j0 = first; j0 < count; j0 += rows * kMoveRows) {
-        uint4 x[kMoveRows];
-        int64_t to[kMoveRows];
+    // with pages in one line the slot's number is its place; with others its page and place are taken apart again
+    const bool line = p.c.page_stride == p.c.page * p.c.slot_stride;
+    auto place = [&](int g) {
+        if (line) return g * p.c.slot_stride;
+        const int id = g / p.c.page;
+        return id * p.c.page_stride + (int64_t)(g - id * p.c.page) * p.c.slot_stride;
+    };
+    for (int base_j = first; base_j < count; base_j += kMoveAhead) {
+        const int n = min(kMoveAhead, count - base_j);
+        for (int i = tid; i < n; i += kMoveThreads) {
+            const int j = base_j + i, s = kept[j], ps = s / p.c.page, pj = j / p.c.page;
+            const int is = table[ps], ij = table[pj];
+            const bool ok = is >= 0 && is < p.c.pages && ij >= 0 && ij < p.c.pages;
+            from[i] = ok ? is * p.c.page + (s - ps * p.c.page) : -1;
+            to[i] = ij * p.c.page + (j - pj * p.c.page);
+        }
+        __syncthreads();
+        for (int i0 = 0; i0 < n; i0 += rows * kMoveRows) {
+            uint4 x[kMoveRows];
 #pragma unroll
-        for (int i = 0; i < kMoveRows; ++i) {
-            const int j = j0 + i * rows + r0;
-            to[i] = -1;
-            if (j < count) {
-                const int64_t from = slot_at(p.c, b, kept[j]);
-                to[i] = from < 0 ? -1 : slot_at(p.c, b, j);
-                if (to[i] >= 0) x[i] = base[from + u];
+            for (int i = 0; i < kMoveRows; ++i) {
+                const int k = i0 + i * rows + r0;
+                if (k < n && from[k] >= 0) x[i] = base[place(from[k])];
+            }
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < kMoveRows; ++i) {
+                const int k = i0 + i * rows + r0;
+                if (k < n && from[k] >= 0) base[place(to[k])] = x[i];
             }
         }
         __syncthreads();
-#pragma unroll
-        for (int i = 0; i < kMoveRows; ++i)
-            if (to[i] >= 0) base[to[i] + u] = x[i];
     }
 }
 
@@ -289,9 +360,8 @@ int launch_cache_append(const ssd_heads &tree_k, const ssd_heads &tree_v, const 
     p.off = tok_off; p.path = path; p.path_len = path_len;
     p.weight = weight; p.weight_stride = weight_stride; p.weight_cols = weight ? weight_cols : 0;
     p.M = M; p.new_len = new_len; p.status = status;
-    // four units of a row a thread, for the average utterance
-    const int64_t units = (M / B + 1) * 2 * p.c.heads * p.c.units;
-    int64_t parts = (units + 4 * kAppendThreads - 1) / (4 * kAppendThreads);
+    // eight rows a CTA, for the average utterance's nodes
+    int64_t parts = (M / B + 7) / 8;
     const int sms = device_sm_count();
     if (sms <= 0) return SSD_ERR_CUDA;
     const int64_t most = (int64_t)sms * 64 / B;

@@ -34,7 +34,7 @@ struct alignas(64) WeightParams {
 template <int D> struct WShape {
     static constexpr int kBlocks = D / 64;
     static constexpr int kSlotBytes = kBlocks * kBlockBytes;
-    static constexpr int kSlots = D == 128 ? 6 : 8;
+    static constexpr int kSlots = D == 128 ? 3 : 6;                // two CTAs fit a multiprocessor: one's end hides in the other's work
     static constexpr int kBars = kSlots * kSlotBytes;              // full[], empty[], scores[2], free[2]
     static constexpr int kNumBars = 2 * kSlots + 4;
     static constexpr int kWords = kBars + kNumBars * 8;            // tmem address, failed
@@ -42,10 +42,10 @@ template <int D> struct WShape {
     static constexpr int kSums = kLse + 2 * kTile * 4;             // [2][128]
     static constexpr int kBytes = kSums + 2 * kTile * 4;
 };
-static_assert(WShape<128>::kBytes <= 232448, "shared memory");
+static_assert(2 * (WShape<128>::kBytes + 1024) <= 233472 && 2 * (WShape<64>::kBytes + 1024) <= 233472, "shared memory of two CTAs");
 
 template <typename T, int D, bool kCap>
-__global__ void __launch_bounds__(kWarps * 32, 1) cache_weights(const __grid_constant__ WeightParams p) {
+__global__ void __launch_bounds__(kWarps * 32, 2) cache_weights(const __grid_constant__ WeightParams p) {
     using S = WShape<D>;
     extern __shared__ __align__(1024) uint8_t base[];
     const uint32_t smem = smem_u32(base);
@@ -136,6 +136,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) cache_weights(const __grid_con
         if (!ok) words[1] = 1;
     } else if (warp == 9) {
         bool ok = true;
+        const uint32_t tm = uniform(tmem);
         for (int u = 0; u < units && ok; ++u) {
             const int c = u % chunks, s = u & 1, k = u >> 1;
             const int keys = u / chunks * (chunks + 1), q_pos = keys + 1 + c;
@@ -144,14 +145,14 @@ __global__ void __launch_bounds__(kWarps * 32, 1) cache_weights(const __grid_con
             if (k > 0) ok = ok && mbar_wait_bounded(scores_free(s), (k - 1) & 1);
             if (!ok) break;
             tc_fence_after();
-            if (lane == 0) {
-                const int rows = min(p.npt, n - c * p.npt) * p.G;
+            const int rows = uniform(min(p.npt, n - c * p.npt) * p.G);
+            if (elect_one()) {
                 const uint32_t idesc = instruction<T>((rows + 15) / 16 * 16, false);
                 const uint64_t a = operand(slot_at(keys)), q = operand(slot_at(q_pos));
 #pragma unroll
                 for (int x = 0; x < D / 16; ++x) {
                     const int o = (x >> 2) * (kBlockBytes >> 4) + (x & 3) * 2;
-                    mma_ss(tmem + s * kTile, a + o, q + o, idesc, x > 0);
+                    mma_ss(tm + s * kTile, a + o, q + o, idesc, x > 0);
                 }
                 mma_commit(scores_full(s));
                 mma_commit(empty(q_pos % S::kSlots));

@@ -47,7 +47,7 @@ BAD_CACHES = [(dict(dtype=ssd.F32), ssd.ERR_DTYPE), (dict(dtype=9), ssd.ERR_DTYP
               (dict(max_pages=-1), ssd.ERR_ARG), (dict(table_stride=2), ssd.ERR_ARG), (dict(len=0), ssd.ERR_NULL),
               (dict(page_table=0), ssd.ERR_NULL), (dict(k=0), ssd.ERR_NULL), (dict(k=264), ssd.ERR_ALIGN),
               (dict(slot_stride=132), ssd.ERR_ALIGN), (dict(head_stride=68), ssd.ERR_ALIGN), (dict(page_stride=2052), ssd.ERR_ALIGN),
-              (dict(page_stride=-8), ssd.ERR_ARG), (dict(page_stride=1 << 40), ssd.ERR_ARG)]
+              (dict(page_stride=-8), ssd.ERR_ARG), (dict(pages=1 << 28, page_size=8), ssd.ERR_ARG), (dict(page_stride=1 << 40), ssd.ERR_ARG)]
 
 
 @pytest.mark.parametrize("kw,code", BAD_CACHES + [(dict(v=0), ssd.ERR_NULL), (dict(v=264), ssd.ERR_ALIGN)])
