@@ -2,6 +2,8 @@
 // values enter it (ssd_cache_append), and slots that have received little attention leave it
 // (ssd_cache_evict).  Copies and integer work, bound by HBM, and by the chain of look-ups (offsets,
 // path, page, row) where the call is small.
+#include <math.h>
+
 #include "ssd_common.cuh"
 
 namespace ssd {
@@ -49,9 +51,9 @@ struct AppendParams {
     uint32_t *status;
 };
 
-constexpr int kAppendThreads = 256, kAppendRows = 4;
+constexpr int kAppendThreads = 256, kAppendRows = 4, kAppendPart = 32;      // rows of a CTA, for the average utterance's nodes
 
-__global__ void __launch_bounds__(kAppendThreads) append_kernel(const AppendParams p) {
+__global__ void __launch_bounds__(kAppendThreads, 6) append_kernel(const AppendParams p) {
     pdl_enter();
     const int b = blockIdx.x / p.parts, part = blockIdx.x % p.parts, tid = threadIdx.x;
     const int64_t i0 = p.off[b], i1 = p.off[b + 1];
@@ -114,6 +116,7 @@ struct EvictParams {
     const float *weight;
     int64_t weight_stride;
     int weight_cols, budget, sink, recent;
+    int heads_each;                                    // of a moving CTA; a power of two that divides the heads
     int32_t *kept;
     float *weight_out;
     int64_t out_stride;
@@ -144,8 +147,10 @@ __device__ __forceinline__ int lanes_before(int v) {
 
 // One CTA per utterance: the k-th largest key of the slots between the first `sink` and the last `recent`
 // by four rounds of 8 bits, then the kept slots in order (of equal keys the lowest slots).  A warp has a
-// run of consecutive slots, 32 at a time: up to 16,384 slots their keys stay in registers and are fetched once.
-constexpr int kKeys = 16, kSelectWarps = kSelectThreads / 32;
+// run of consecutive slots, 32 at a time.  Up to 32,768 slots the weights are fetched once, into shared memory; the
+// loops over them are short and not unrolled (held in registers and unrolled, 4,096 slots took 13.6 us, most of
+// it the code's own way into the instruction cache).
+constexpr int kHeld = 32768, kSelectWarps = kSelectThreads / 32;
 
 struct SelectShared {
     int hist[256];
@@ -154,24 +159,13 @@ struct SelectShared {
     unsigned any;
 };
 
-template <bool kHeld>
 __device__ __forceinline__ void select_slots(const EvictParams &p, SelectShared &sh, const float *w, int len, int32_t *kept, float *wout) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int lo = p.sink, hi = len - p.recent, want = p.budget - p.sink - p.recent;
     const int steps = (len + kSelectThreads - 1) / kSelectThreads, mine = warp * steps * 32 + lane;      // + 32 a step
-    float held[kHeld ? kKeys : 1];
-    if (kHeld) {
-#pragma unroll
-        for (int i = 0; i < kKeys; ++i) held[i] = i < steps && mine + i * 32 < len ? w[mine + i * 32] : 0.f;
-    }
     auto each = [&](auto body) {                       // body(slot, weight) for all of this thread's, whole warps at a time
-        if (kHeld) {
-#pragma unroll
-            for (int i = 0; i < kKeys; ++i)
-                if (i < steps) body(mine + i * 32, held[i]);
-        } else {
-            for (int i = 0; i < steps; ++i) body(mine + i * 32, mine + i * 32 < len ? w[mine + i * 32] : 0.f);
-        }
+#pragma unroll 2
+        for (int i = 0; i < steps; ++i) body(mine + i * 32, mine + i * 32 < len ? w[mine + i * 32] : 0.f);
     };
     uint32_t prefix = 0, mask = 0;
     int left = want;                                   // to be taken of the keys that match the prefix
@@ -182,10 +176,14 @@ __device__ __forceinline__ void select_slots(const EvictParams &p, SelectShared 
             each([&](int i, float x) {
                 const uint32_t key = weight_key(x);
                 const bool in = i >= lo && i < hi && (key & mask) == prefix;
-                // weights share their leading bits: lanes with the same digit count as one
                 const uint32_t digit = in ? key >> shift & 255 : 256u;
-                const unsigned same = __match_any_sync(0xffffffffu, digit);
-                if (in && (__ffs(same) - 1) == lane) atomicAdd(&sh.hist[digit], __popc(same));
+                if (shift == 24) {
+                    // weights share their leading bits: lanes with the same digit count as one
+                    const unsigned same = __match_any_sync(0xffffffffu, digit);
+                    if (in && (__ffs(same) - 1) == lane) atomicAdd(&sh.hist[digit], __popc(same));
+                } else if (in) {
+                    atomicAdd(&sh.hist[digit], 1);
+                }
             });
             __syncthreads();
             if (tid < 32) {                            // the digit at which the count from above reaches `left`
@@ -250,7 +248,8 @@ __device__ __forceinline__ void select_slots(const EvictParams &p, SelectShared 
     });
 }
 
-__global__ void __launch_bounds__(kSelectThreads) select_kernel(const EvictParams p) {
+__global__ void __launch_bounds__(kSelectThreads) select_kernel(const EvictParams p, int held) {
+    extern __shared__ float weights_here[];
     __shared__ SelectShared sh;
     pdl_enter();
     const int b = blockIdx.x, tid = threadIdx.x;
@@ -280,10 +279,14 @@ __global__ void __launch_bounds__(kSelectThreads) select_kernel(const EvictParam
             kept[j] = j;
             if (wout) wout[j] = j < p.weight_cols ? w[j] : 0.f;
         }
-    } else if (len <= kKeys * kSelectThreads) {
-        select_slots<true>(p, sh, w, len, kept, wout);
     } else {
-        select_slots<false>(p, sh, w, len, kept, wout);
+        const float *at = w;
+        if (len <= held) {
+            for (int i = tid; i < len; i += kSelectThreads) weights_here[i] = w[i];
+            at = weights_here;
+            __syncthreads();
+        }
+        select_slots(p, sh, at, len, kept, wout);
     }
     __syncthreads();
     if (tid == 0) { p.new_len[b] = count; p.status[b] = sh.any; }
@@ -292,25 +295,20 @@ __global__ void __launch_bounds__(kSelectThreads) select_kernel(const EvictParam
 // Kept slots move down in order, kept[j] to j.  kept[j] >= j, and ascending, so a block of slots may be
 // written once all of its own sources have been read: later blocks' sources lie behind it.
 // Where slots lie is looked up for a thousand rows ahead, so that a block of rows costs one round trip.
-constexpr int kMoveThreads = 256, kMoveRows = 8, kMoveAhead = 1024;
+constexpr int kMoveThreads = 512, kMoveRows = 8, kMoveAhead = 1024;
 
-__global__ void __launch_bounds__(kMoveThreads) move_kernel(const EvictParams p) {
+__global__ void __launch_bounds__(kMoveThreads, 2) move_kernel(const EvictParams p) {
     // slot numbers over all pages (page id times page size and the slot in it), or -1
     __shared__ int from[kMoveAhead], to[kMoveAhead];
     pdl_enter();
-    const int kv = blockIdx.x & 1, h = blockIdx.x / 2 % p.c.heads, b = blockIdx.x / 2 / p.c.heads, tid = threadIdx.x;
+    const int kv = blockIdx.x & 1, groups = p.c.heads / p.heads_each, h = blockIdx.x / 2 % groups * p.heads_each;
+    const int b = blockIdx.x / 2 / groups, tid = threadIdx.x;
     const int count = p.new_len[b];
     const int32_t *const kept = p.kept + (int64_t)b * p.budget;
     const int32_t *const table = p.c.table + b * p.c.table_stride;
-    const int u = tid % p.c.units, r0 = tid / p.c.units, rows = kMoveThreads / p.c.units;
-    uint4 *const base = (kv ? p.c.v : p.c.k) + h * p.c.head_stride + u;
-    // slots before the first gap stay: kept[j] == j holds up to there and nowhere behind
-    if (count == 0 || kept[count - 1] == count - 1) return;
-    int first = 0, end = count;
-    while (first < end) {
-        const int mid = (first + end) >> 1;
-        if (kept[mid] == mid) first = mid + 1; else end = mid;
-    }
+    const int width = p.heads_each * p.c.units, u = tid % width, r0 = tid / width, rows = kMoveThreads / width;
+    uint4 *const base = (kv ? p.c.v : p.c.k) + (h + u / p.c.units) * p.c.head_stride + u % p.c.units;
+    if (count == 0 || kept[count - 1] == count - 1) return;      // every slot stays where it is
     // with pages in one line the slot's number is its place; with others its page and place are taken apart again
     const bool line = p.c.page_stride == p.c.page * p.c.slot_stride;
     auto place = [&](int g) {
@@ -318,12 +316,12 @@ __global__ void __launch_bounds__(kMoveThreads) move_kernel(const EvictParams p)
         const int id = g / p.c.page;
         return id * p.c.page_stride + (int64_t)(g - id * p.c.page) * p.c.slot_stride;
     };
-    for (int base_j = first; base_j < count; base_j += kMoveAhead) {
+    for (int base_j = 0; base_j < count; base_j += kMoveAhead) {
         const int n = min(kMoveAhead, count - base_j);
         for (int i = tid; i < n; i += kMoveThreads) {
             const int j = base_j + i, s = kept[j], ps = s / p.c.page, pj = j / p.c.page;
             const int is = table[ps], ij = table[pj];
-            const bool ok = is >= 0 && is < p.c.pages && ij >= 0 && ij < p.c.pages;
+            const bool ok = s != j && is >= 0 && is < p.c.pages && ij >= 0 && ij < p.c.pages;      // slots before the first gap stay
             from[i] = ok ? is * p.c.page + (s - ps * p.c.page) : -1;
             to[i] = ij * p.c.page + (j - pj * p.c.page);
         }
@@ -360,8 +358,7 @@ int launch_cache_append(const ssd_heads &tree_k, const ssd_heads &tree_v, const 
     p.off = tok_off; p.path = path; p.path_len = path_len;
     p.weight = weight; p.weight_stride = weight_stride; p.weight_cols = weight ? weight_cols : 0;
     p.M = M; p.new_len = new_len; p.status = status;
-    // eight rows a CTA, for the average utterance's nodes
-    int64_t parts = (M / B + 7) / 8;
+    int64_t parts = (M / B + kAppendPart - 1) / kAppendPart;
     const int sms = device_sm_count();
     if (sms <= 0) return SSD_ERR_CUDA;
     const int64_t most = (int64_t)sms * 64 / B;
@@ -384,9 +381,29 @@ int launch_cache_evict(const ssd_kv_cache &cache, const float *weight, int64_t w
     p.weight = weight; p.weight_stride = weight_stride; p.weight_cols = weight_cols;
     p.budget = budget; p.sink = sink; p.recent = recent;
     p.kept = kept; p.weight_out = weight_out; p.out_stride = out_stride; p.new_len = new_len; p.status = status;
-    const int64_t grid = 2ll * p.c.heads * B;
+    // A CTA moves as many heads of a slot as do not leave the last round of CTAs (two to a multiprocessor) a tenth
+    // emptier than the best: DRAM likes rows of 1 KB better than of 256 B (64 caches of 8 heads: 227 us a head
+    // each, 212 four), 200 caches are better off with 800 CTAs than with 400 (466 us, 513).
+    const int sms = device_sm_count();
+    if (sms <= 0) return SSD_ERR_CUDA;
+    auto filled = [&](int each) {
+        const double rounds = 2.0 * B * (p.c.heads / each) / (2.0 * sms);
+        return rounds / ceil(rounds);
+    };
+    double best = 0.0;
+    p.heads_each = 1;
+    for (int pass = 0; pass < 2; ++pass)
+        for (int each = 1; p.c.heads % each == 0 && each * p.c.units <= kMoveThreads; each *= 2) {
+            if (pass == 0) best = filled(each) > best ? filled(each) : best;
+            else if (filled(each) >= 0.9 * best) p.heads_each = each;
+        }
+    const int64_t grid = 2ll * (p.c.heads / p.heads_each) * B;
     if (grid > INT32_MAX) return SSD_ERR_ARG;
-    cudaError_t e = launch_pdl(select_kernel, (unsigned)B, (unsigned)kSelectThreads, 0, stream, p);
+    // no more shared memory than the longest cache can need
+    const int64_t room = (int64_t)p.c.max_pages * p.c.page, most = room < weight_cols ? room : weight_cols;
+    const int held = most <= kHeld ? (int)most : kHeld;
+    cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void *>(select_kernel), (size_t)held * 4);
+    if (e == cudaSuccess) e = launch_pdl(select_kernel, (unsigned)B, (unsigned)kSelectThreads, (size_t)held * 4, stream, p, held);
     if (e == cudaSuccess && p.c.pages > 0) e = launch_pdl(move_kernel, (unsigned)grid, (unsigned)kMoveThreads, 0, stream, p);
     if (e == cudaSuccess) e = cudaGetLastError();
     if (e != cudaSuccess) { record_cuda_error(e); return SSD_ERR_CUDA; }

@@ -120,10 +120,12 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cache_weights(const __grid_con
         for (int k = 0; k < heads && ok; ++k) {
             const int h = rank + k * p.split;
             if (!take(copies * box * 128 * S::kBlocks)) break;
-            for (int i = 0; i < copies; ++i) {
+            {
+                // copies are of 64 columns and 8 rows at least: a lane for each
+                const int i = lane / S::kBlocks, x = lane % S::kBlocks;
                 const int page = __shfl_sync(0xffffffffu, id, p.paging.pages ? i : 0);
-                if (lane < S::kBlocks)
-                    tma_load_4d(slot_at(pos) + lane * kBlockBytes + i * box * 128, &p.cache_k, lane * 64, h,
+                if (i < copies)
+                    tma_load_4d(slot_at(pos) + x * kBlockBytes + i * box * 128, &p.cache_k, x * 64, h,
                                 p.paging.pages ? 0 : at.slot + i * box, page, full(pos % S::kSlots));
             }
             ++pos;

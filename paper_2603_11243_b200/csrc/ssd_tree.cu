@@ -81,7 +81,7 @@ static_assert(Shape<128>::kBytes <= 232448, "shared memory");
 // ---- the line of key tiles and its cuts -----------------------------------------------------------
 // A tile costs as much as it has tiles of queries, 2,400 clocks each; an item's end costs 6,000 to 8,000 (its last products
 // are waited for, its results written).
-constexpr int kEndCost = 3;
+constexpr int kEndCost = 3, kLeastPart = 2;
 struct Utterance {
     int64_t i0;
     int n, len, cache_tiles, q_items;
@@ -175,8 +175,11 @@ struct Walk {
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
         total *= p.Hkv;
-        lo = scaled(total, blockIdx.x, gridDim.x);
-        hi = scaled(total, blockIdx.x + 1, gridDim.x);
+        // parts of at least kLeastPart: what a short one saves, the closing kernel spends on joining it
+        const int parts = (int)min((int64_t)gridDim.x, max(total / kLeastPart, (int64_t)1));
+        if ((int)blockIdx.x >= parts) return false;
+        lo = scaled(total, blockIdx.x, parts);
+        hi = scaled(total, blockIdx.x + 1, parts);
         if (lo >= hi) return false;
         int64_t before = 0;
         for (int i0 = 0; i0 < p.B; i0 += 32) {
