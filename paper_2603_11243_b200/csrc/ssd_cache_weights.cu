@@ -26,23 +26,27 @@ struct alignas(64) WeightParams {
     float *weight;
     uint32_t *status;
     int64_t table_stride, weight_stride, M;
-    int Hq, Hkv, G, npt, max_nodes, n_pages, max_pages, weight_cols, tiles, split;
+    int Hq, Hkv, G, npt, q_rows, max_nodes, n_pages, max_pages, weight_cols, tiles, split;
     Paging paging;
     float scale, cap;
 };
 
+// Keys and queries have slots of their own: a head's keys stay while its tiles of queries pass, however many.
 template <int D> struct WShape {
     static constexpr int kBlocks = D / 64;
-    static constexpr int kSlotBytes = kBlocks * kBlockBytes;
-    static constexpr int kSlots = D == 128 ? 3 : 6;                // two CTAs fit a multiprocessor: one's end hides in the other's work
-    static constexpr int kBars = kSlots * kSlotBytes;              // full[], empty[], scores[2], free[2]
-    static constexpr int kNumBars = 2 * kSlots + 4;
+    static constexpr int kKeyBytes = kBlocks * kBlockBytes, kKeySlots = D == 128 ? 2 : 4;
+    static constexpr int kQueries = kKeySlots * kKeyBytes, kQueryBytes = 32768;      // two tiles, or one of more than 64 rows of 128
+    static constexpr int kBars = kQueries + kQueryBytes;           // keys full[], empty[], queries full[2], empty[2], scores[2], free[2]
+    static constexpr int kNumBars = 2 * kKeySlots + 8;
     static constexpr int kWords = kBars + kNumBars * 8;            // tmem address, failed
-    static constexpr int kLse = (kWords + 8 + 15) / 16 * 16;       // [2][128], times log2 e
-    static constexpr int kSums = kLse + 2 * kTile * 4;             // [2][128]
+    static constexpr int kLse = (kWords + 8 + 15) / 16 * 16;       // [8][128], times log2 e: a warp's own, so that none waits
+    static constexpr int kSums = kLse + 8 * kTile * 4;             // for another; [2][128]
     static constexpr int kBytes = kSums + 2 * kTile * 4;
 };
+// two CTAs fit a multiprocessor: one's end hides in the other's work
 static_assert(2 * (WShape<128>::kBytes + 1024) <= 233472 && 2 * (WShape<64>::kBytes + 1024) <= 233472, "shared memory of two CTAs");
+// Rows of a tile of queries: 64 where two such tiles take the place of one of 128.
+inline int query_rows(int D, int G) { return D == 128 && G <= 64 ? 64 : kTile; }
 
 template <typename T, int D, bool kCap>
 __global__ void __launch_bounds__(kWarps * 32, 2) cache_weights(const __grid_constant__ WeightParams p) {
@@ -79,18 +83,28 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cache_weights(const __grid_con
     const int heads = (p.Hkv - rank + p.split - 1) / p.split;    // of this CTA: rank, rank + split, ...
     const int units = heads * chunks;
 
-    auto full = [&](int i) { return smem + S::kBars + 8 * i; };
-    auto empty = [&](int i) { return smem + S::kBars + 8 * (S::kSlots + i); };
-    auto scores_full = [&](int s) { return smem + S::kBars + 8 * (2 * S::kSlots + s); };
-    auto scores_free = [&](int s) { return smem + S::kBars + 8 * (2 * S::kSlots + 2 + s); };
+    const int q_slots = p.q_rows * 128 * S::kBlocks * 2 <= S::kQueryBytes ? 2 : 1, q_block = p.q_rows * 128;
+    const uint32_t bars = smem + S::kBars, more = bars + 16 * S::kKeySlots;
+    auto keys_full = [&](int k) { return bars + 8 * (k % S::kKeySlots); };
+    auto keys_empty = [&](int k) { return bars + 8 * (S::kKeySlots + k % S::kKeySlots); };
+    auto q_full = [&](int i) { return more + 8 * i; };
+    auto q_empty = [&](int i) { return more + 16 + 8 * i; };
+    auto scores_full = [&](int s) { return more + 32 + 8 * s; };
+    auto scores_free = [&](int s) { return more + 48 + 8 * s; };
     volatile uint32_t *const words = reinterpret_cast<volatile uint32_t *>(base + S::kWords);
     float *const sums = reinterpret_cast<float *>(base + S::kSums);
-    auto slot_at = [&](int pos) { return smem + (pos % S::kSlots) * S::kSlotBytes; };
+    auto keys_at = [&](int k) { return smem + (k % S::kKeySlots) * S::kKeyBytes; };
+    auto q_at = [&](int i) { return smem + S::kQueries + i * S::kBlocks * q_block; };
 
     if (warp == 8) tmem_alloc(smem + S::kWords, 256);
     if (tid == 0) {
-        for (int i = 0; i < S::kSlots; ++i) { mbar_init(full(i), 1); mbar_init(empty(i), 1); }
-        for (int s = 0; s < 2; ++s) { mbar_init(scores_full(s), 1); mbar_init(scores_free(s), 4); }
+        for (int i = 0; i < S::kKeySlots; ++i) { mbar_init(keys_full(i), 1); mbar_init(keys_empty(i), 1); }
+        for (int s = 0; s < 2; ++s) {
+            mbar_init(q_full(s), 1);
+            mbar_init(q_empty(s), 1);
+            mbar_init(scores_full(s), 1);
+            mbar_init(scores_free(s), 4);
+        }
         mbar_init_fence();
         words[1] = 0;
     }
@@ -101,7 +115,6 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cache_weights(const __grid_con
     const uint32_t tmem = words[0];
 
     if (warp == 8) {
-        // a head's keys, then its tiles of queries
         const int page_count = p.paging.pages ? p.paging.pages : 1;
         int id = p.n_pages;                                      // outside: the copy fills in zeros
         if (lane < page_count && at.page + lane < p.max_pages) {
@@ -109,30 +122,33 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cache_weights(const __grid_con
             if (id < 0 || id >= p.n_pages) id = p.n_pages;
         }
         const int box = p.paging.box, copies = (at.valid + box - 1) / box;
+        // copies are of 64 columns and 8 rows at least: a lane for each
+        const int i = lane / S::kBlocks, x = lane % S::kBlocks;
+        const int page = __shfl_sync(0xffffffffu, id, p.paging.pages ? i : 0);
         bool ok = true;
-        int pos = 0;
-        auto take = [&](int bytes) {
-            if (pos >= S::kSlots) ok = mbar_wait_bounded(empty(pos % S::kSlots), (pos / S::kSlots - 1) & 1);
-            if (ok && lane == 0) mbar_arrive_expect_tx(full(pos % S::kSlots), bytes);
+        auto keys = [&](int k) {
+            if (k >= S::kKeySlots) ok = ok && mbar_wait_bounded(keys_empty(k), (k / S::kKeySlots - 1) & 1);
+            if (!ok) return;
+            if (lane == 0) mbar_arrive_expect_tx(keys_full(k), copies * box * 128 * S::kBlocks);
             __syncwarp();
-            return ok;
+            if (i < copies)
+                tma_load_4d(keys_at(k) + x * kBlockBytes + i * box * 128, &p.cache_k, x * 64, rank + k * p.split,
+                            p.paging.pages ? 0 : at.slot + i * box, page, keys_full(k));
         };
-        for (int k = 0; k < heads && ok; ++k) {
-            const int h = rank + k * p.split;
-            if (!take(copies * box * 128 * S::kBlocks)) break;
-            {
-                // copies are of 64 columns and 8 rows at least: a lane for each
-                const int i = lane / S::kBlocks, x = lane % S::kBlocks;
-                const int page = __shfl_sync(0xffffffffu, id, p.paging.pages ? i : 0);
-                if (i < copies)
-                    tma_load_4d(slot_at(pos) + x * kBlockBytes + i * box * 128, &p.cache_k, x * 64, h,
-                                p.paging.pages ? 0 : at.slot + i * box, page, full(pos % S::kSlots));
-            }
-            ++pos;
-            for (int c = 0; c < chunks; ++c, ++pos) {
-                if (!take(p.G * p.npt * 128 * S::kBlocks)) break;
+        // Later heads' keys are asked for when the head that had their slot is as good as done: its last queries are
+        // under way, and so are the next head's first.
+        int ahead = 0;
+        for (; ahead < heads && ahead < S::kKeySlots; ++ahead) keys(ahead);
+        for (int k = 0, u = 0; k < heads && ok; ++k) {
+            for (int c = 0; c < chunks && ok; ++c, ++u) {
+                const int q = u % q_slots;
+                if (u >= q_slots) ok = mbar_wait_bounded(q_empty(q), (u / q_slots - 1) & 1);
+                if (!ok) break;
+                if (lane == 0) mbar_arrive_expect_tx(q_full(q), p.G * p.npt * 128 * S::kBlocks);
+                __syncwarp();
                 if (lane < S::kBlocks)
-                    tma_load_3d(slot_at(pos) + lane * kBlockBytes, &p.q, lane * 64, h * p.G, (int)i0 + c * p.npt, full(pos % S::kSlots));
+                    tma_load_3d(q_at(q) + lane * q_block, &p.q, lane * 64, (rank + k * p.split) * p.G, (int)i0 + c * p.npt, q_full(q));
+                if (c == 0 && k > 0 && ahead < heads) keys(ahead++);
             }
         }
         if (!ok) words[1] = 1;
@@ -140,25 +156,22 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cache_weights(const __grid_con
         bool ok = true;
         const uint32_t tm = uniform(tmem);
         for (int u = 0; u < units && ok; ++u) {
-            const int c = u % chunks, s = u & 1, k = u >> 1;
-            const int keys = u / chunks * (chunks + 1), q_pos = keys + 1 + c;
-            ok = mbar_wait_bounded(full(keys % S::kSlots), (keys / S::kSlots) & 1) &&
-                 mbar_wait_bounded(full(q_pos % S::kSlots), (q_pos / S::kSlots) & 1);
-            if (k > 0) ok = ok && mbar_wait_bounded(scores_free(s), (k - 1) & 1);
+            const int k = u / chunks, c = u - k * chunks, s = u & 1, q = u % q_slots;
+            ok = mbar_wait_bounded(keys_full(k), (k / S::kKeySlots) & 1) && mbar_wait_bounded(q_full(q), (u / q_slots) & 1);
+            if (u > 1) ok = ok && mbar_wait_bounded(scores_free(s), ((u >> 1) - 1) & 1);
             if (!ok) break;
             tc_fence_after();
             const int rows = uniform(min(p.npt, n - c * p.npt) * p.G);
             if (elect_one()) {
                 const uint32_t idesc = instruction<T>((rows + 15) / 16 * 16, false);
-                const uint64_t a = operand(slot_at(keys)), q = operand(slot_at(q_pos));
+                const uint64_t a = operand(keys_at(k)), b = operand(q_at(q));
 #pragma unroll
-                for (int x = 0; x < D / 16; ++x) {
-                    const int o = (x >> 2) * (kBlockBytes >> 4) + (x & 3) * 2;
-                    mma_ss(tm + s * kTile, a + o, q + o, idesc, x > 0);
-                }
+                for (int x = 0; x < D / 16; ++x)
+                    mma_ss(tm + s * kTile, a + (x >> 2) * (kBlockBytes >> 4) + (x & 3) * 2, b + (x >> 2) * (q_block >> 4) + (x & 3) * 2,
+                           idesc, x > 0);
                 mma_commit(scores_full(s));
-                mma_commit(empty(q_pos % S::kSlots));
-                if (c == chunks - 1) mma_commit(empty(keys % S::kSlots));
+                mma_commit(q_empty(q));
+                if (c == chunks - 1) mma_commit(keys_empty(k));
             }
             __syncwarp();
         }
@@ -166,7 +179,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cache_weights(const __grid_con
     } else {
         const int s = warp >> 2, row = (warp & 3) * 32 + lane;
         const uint32_t t_scores = tmem + s * kTile + ((uint32_t)((warp & 3) * 32) << 16);
-        float *const lse = reinterpret_cast<float *>(base + S::kLse) + s * kTile;
+        float *const lse = reinterpret_cast<float *>(base + S::kLse) + warp * kTile;
         const bool busy = (warp & 3) * 32 < at.valid;
         const float c = kCap ? kLog2e : p.scale * kLog2e;
         float sum = 0.f;
@@ -174,14 +187,16 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cache_weights(const __grid_con
         for (int u = s; u < units; u += 2) {
             const int chunk = u % chunks, h = rank + u / chunks * p.split, k = u >> 1;
             const int rows = min(p.npt, n - chunk * p.npt) * p.G;
-            named_sync(1 + s, 128);                              // everyone is done with the last unit's
-            {
-                const int64_t node = i0 + chunk * p.npt + row / p.G;
-                float x = INFINITY;                              // not counted: the probability is 0
-                if (row < rows && (!p.use || p.use[node])) x = p.lse[node * p.Hq + h * p.G + row % p.G] * kLog2e;
-                lse[row] = x;
+            if (busy) {
+                __syncwarp();                                    // the last unit's are read
+                for (int r = lane; r < (rows + 15) / 16 * 16; r += 32) {
+                    float x = INFINITY;                          // not counted: the probability is 0
+                    const int64_t node = i0 + chunk * p.npt + r / p.G;
+                    if (r < rows && (!p.use || p.use[node])) x = p.lse[node * p.Hq + h * p.G + r % p.G] * kLog2e;
+                    lse[r] = x;
+                }
+                __syncwarp();
             }
-            named_sync(1 + s, 128);
             ok = mbar_wait_bounded(scores_full(s), k & 1);
             if (!ok) break;
             tc_fence_after();
@@ -259,7 +274,8 @@ int launch_cache_weights(const ssd_heads &q, const float *lse, const ssd_kv_cach
     WeightParams p;
     p.paging = paging(cache.page_size);
     p.G = q.heads / cache.heads;
-    p.npt = kTile / p.G;
+    p.q_rows = query_rows(cache.head_dim, p.G);
+    p.npt = p.q_rows / p.G;
     if (p.npt > max_nodes) p.npt = max_nodes > 0 ? max_nodes : 1;
     const int D = cache.head_dim;
     if (M > 0 && !encode_rows(&p.q, cache.dtype, q, D, M, p.G, p.npt)) return SSD_ERR_CUDA;

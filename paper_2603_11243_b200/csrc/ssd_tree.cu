@@ -67,7 +67,7 @@ template <int D> struct Shape {
     static constexpr int kRing = 2 * kSlotBytes;                  // behind the two tiles of queries
     static constexpr int kMisc = kRing + kSlots * kSlotBytes;
     static constexpr int kBars = kMisc;     // full[], empty[], q full[2], q empty[2], scores[2], probs[2], sums[2], sums free
-    static constexpr int kNumBars = 2 * kSlots + 15;              // and segments full[2], empty[2]
+    static constexpr int kNumBars = 2 * kSlots + 16;              // and segments full[2], empty[2], softmax warps together
     static constexpr int kWords = kBars + kNumBars * 8;           // tmem address, failed, bad value seen [2]
     static constexpr int kMl = (kWords + 16 + 15) / 16 * 16;      // [2][128] running maximum and sum
     static constexpr int kParent = kMl + 2 * kTile * 8;
@@ -339,6 +339,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
     const uint32_t sums_free = more + 80;
     auto segment_full = [&](int i) { return more + 88 + 8 * i; };
     auto segment_empty = [&](int i) { return more + 104 + 8 * i; };
+    const uint32_t together = more + 120;
     volatile Segment *const ring = reinterpret_cast<volatile Segment *>(base + S::kSegments);
     volatile uint32_t *const words = reinterpret_cast<volatile uint32_t *>(base + S::kWords);
     volatile uint32_t *const failed = words + 1;
@@ -360,6 +361,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
             mbar_init(segment_empty(s), 11);
         }
         mbar_init(sums_free, 8);
+        mbar_init(together, 8);
         mbar_init_fence();
         words[1] = words[2] = words[3] = 0;
     }
@@ -563,6 +565,14 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
         none.last_b = -1;
         p.cuts[blockIdx.x] = none;
     }
+    // The eight softmax warps wait for one another, with a limit as every wait here: a warp that has given up
+    // keeps nobody.
+    int meetings = 0;
+    auto meet = [&] {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(together);
+        ok = ok && mbar_wait_bounded(together, meetings++ & 1);
+    };
     for (int g = 0; take(g, ok); give(g++)) {
         const volatile Segment &w = ring[g & 1];
         const int pair = w.pair, begin = w.begin, tiles = w.end - begin;
@@ -597,7 +607,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
                 const int up = p.parent[w.i0 + j];
                 parents[j] = (int16_t)(up < -1 || up >= j ? -1 : up);
             }
-            named_sync(1, 256);
+            meet();
         }
         int walk = live ? node : -1;
         float m = -INFINITY, l = 0.f;
@@ -722,7 +732,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
                 ++closed[i];
             }
         if (!ok) *failed = 1;
-        named_sync(1, 256);
+        meet();
         tc_fence_after();
         const bool sick = *seen != 0;
         // a pair of tiles: this stream's sums; else the two streams' of one tile, half the columns each
@@ -810,7 +820,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
             if (g == 0) cut.first_b = w.b;
             cut.last_b = w.b;
         }
-        named_sync(1, 256);                          // everyone is done with ml, parents and seen
+        meet();                                      // everyone is done with ml, parents and seen
         if (tid == 0) *seen = 0;
     }
     if (!ok) *failed = 1;

@@ -120,6 +120,18 @@ def test_weights(cuda_device, dtype, cap, n, lens, Hq, Hkv, D, page):
         assert torch.equal(again, got + got)
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n,Hq,Hkv", [([300, 7, 65], 4, 2), ([33, 130], 16, 2), ([9, 17], 96, 1), ([5, 40], 128, 1), ([200], 3, 1)])
+def test_weights_of_many_tiles_of_queries(cuda_device, D, n, Hq, Hkv):
+    """More tiles of queries to a head than slots for them: its keys have to stay, and nobody may wait for them to go."""
+    c = Case(29, n, [150 + 20 * i for i in range(len(n))], Hq=Hq, Hkv=Hkv, D=D, chain=True)
+    lse = c.attention()[1].float()
+    got, status = run_weights(c, cuda_device, lse)
+    want = weights(c, lse, None, 0.0)
+    assert not status.any()
+    assert ((got.cpu().double() - want).abs() <= 1e-5 * want + 1e-12).all()
+
+
 def test_weights_of_uncounted_nodes_and_short_arrays(cuda_device):
     c = Case(23, [7, 40], [300, 150])
     lse = c.attention()[1].float()
