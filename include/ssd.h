@@ -411,7 +411,8 @@ int32_t ssd_verify_combine(const float *stats_all, int32_t R, int64_t V_total,
  *
  * Keys, values, queries and attention outputs are SSD_BF16 or SSD_F16, heads are 64 or 128 values
  * long and contiguous; every base address and every stride of an axis with more than one entry is a
- * multiple of 16 bytes (else SSD_ERR_ALIGN).  Strides count elements.  A cache has at most 2^31 - 1 slots.
+ * multiple of 16 bytes (else SSD_ERR_ALIGN).  Strides count elements.  A cache has at most 2^31 - 1
+ * slots, an utterance at most 2^31 - 257.
  */
 typedef struct ssd_heads {     /* an array [M, heads, head_dim] */
     void *data;

@@ -27,7 +27,7 @@ CacheParams cache_params(const ssd_kv_cache &c) {
 }
 __device__ __forceinline__ int64_t room_of(const CacheParams &c) {
     const int64_t room = (int64_t)c.max_pages * c.page;
-    return room < INT32_MAX ? room : INT32_MAX;
+    return room < INT32_MAX - 256 ? room : INT32_MAX - 256;      // as the attention has it
 }
 // Where slot s of utterance b lies, in units from the cache's base; -1: its page is none of the cache's.
 __device__ __forceinline__ int64_t slot_at(const CacheParams &c, int b, int s) {

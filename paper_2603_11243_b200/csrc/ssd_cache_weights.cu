@@ -61,7 +61,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cache_weights(const __grid_con
     const bool rows_ok = !(i0 < 0 || i1 < i0 || i1 > p.M || i1 - i0 > p.max_nodes);
     const int n = rows_ok ? (int)(i1 - i0) : 0;
     const int64_t room = (int64_t)p.max_pages * p.paging.page;
-    const int most = (int)min(min(room, (int64_t)p.weight_cols), (int64_t)INT32_MAX);
+    const int most = (int)min(min(room, (int64_t)p.weight_cols), kMostSlots);
     const int len = min(max(given, 0), most);
     if (tile == 0 && rank == 0 && warp == 0) {
         uint32_t bits = rows_ok ? 0u : SSD_UTT_BAD_OFFSETS;
@@ -289,7 +289,7 @@ int launch_cache_weights(const ssd_heads &q, const float *lse, const ssd_kv_cach
     if (sms <= 0) return SSD_ERR_CUDA;
     int64_t room = (int64_t)p.max_pages * cache.page_size;
     if (room > weight_cols) room = weight_cols;
-    const int64_t tiles = paged_tiles(p.paging, (int)(room < INT32_MAX - 2 * kTile ? room : INT32_MAX - 2 * kTile));
+    const int64_t tiles = paged_tiles(p.paging, (int)(room < kMostSlots ? room : kMostSlots));
     p.tiles = tiles > 0 ? (int)tiles : 1;
     p.split = 1;
     while (p.split < 8 && p.split * 2 <= p.Hkv && (int64_t)B * p.tiles * p.split * 2 <= 2 * sms) p.split *= 2;

@@ -157,15 +157,14 @@ template <> __device__ __forceinline__ uint32_t pack2<__half>(float lo, float hi
     return r;
 }
 // x -> cap tanh(scale x / cap) of N scores a thread.  Scores well below the cap, as nearly all are, take an odd
-// polynomial (tanh(y) / y in y^2 on |y| <= 1/2, least maximum relative error by Remez's exchange: 1.3e-8): five
+// polynomial (tanh(y) / y in y^2 on |y| <= 1/2, least maximum relative error by Remez's exchange: 1.3e-8): eight
 // packed operations for two scores and none on the special-function unit, which the softmax needs.  Where a
 // score of the warp is larger, y >= 1/2 goes through 1 - 2 / (1 + e^2y): its error, 1e-7, is then relative to
 // at least 0.46.
 // `counts`: whether the thread's scores are anybody's (what lies in other rows must not send a warp the long way).
 template <int N> __device__ __forceinline__ void cap_scores(float *x, float scale, float cap, bool counts) {
-    const float r = scale / cap, r2 = r * r;
-    const float c1 = -0.33333069394019127f * r2, c2 = 0.13324779317551644f * r2 * r2, c3 = -0.05298607528769192f * r2 * r2 * r2,
-                c4 = 0.01713500662684319f * (r2 * r2) * (r2 * r2);
+    const float r = scale / cap;
+    constexpr float c1 = -0.33333069394019127f, c2 = 0.13324779317551644f, c3 = -0.05298607528769192f, c4 = 0.01713500662684319f;
     float top[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < N; i += 8)
@@ -173,12 +172,12 @@ template <int N> __device__ __forceinline__ void cap_scores(float *x, float scal
         for (int k = 0; k < 4; ++k) top[k] = fmaxf(fmaxf(top[k], fabsf(x[i + k])), fabsf(x[i + 4 + k]));      // NaN stays NaN either way
     const bool all_small = __all_sync(0xffffffffu, !counts || fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * r <= 0.5f);
     auto poly = [&](float2 v) {
-        const float2 t = fmul2(v, v);
+        const float2 y = fmul2(v, make_float2(r, r)), t = fmul2(y, y);
         float2 q = ffma2(make_float2(c4, c4), t, make_float2(c3, c3));
         q = ffma2(q, t, make_float2(c2, c2));
         q = ffma2(q, t, make_float2(c1, c1));
         q = ffma2(q, t, make_float2(1.f, 1.f));
-        return fmul2(q, fmul2(v, make_float2(scale, scale)));
+        return fmul2(q, fmul2(y, make_float2(cap, cap)));
     };
     if (all_small) {
 #pragma unroll
@@ -228,6 +227,7 @@ inline Paging paging(int page) {
     }
     return p;
 }
+constexpr int64_t kMostSlots = INT32_MAX - 256;      // of an utterance, so that rounding up to tiles stays in 32 bits
 struct TileAt {
     int page, slot, valid;    // first page (of the utterance's table), first slot in it, slots that count
 };

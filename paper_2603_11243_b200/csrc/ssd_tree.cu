@@ -27,7 +27,7 @@ namespace {
 
 using namespace tc;
 
-constexpr int kWarps = 12;
+constexpr int kWarps = 12, kLaunchRegisters = 168;
 constexpr int kParents = 256;            // parents kept in shared memory; more are read from global
 constexpr int kTreeBox = 16;             // nodes that one copy brings
 
@@ -94,7 +94,7 @@ __device__ __forceinline__ Utterance utterance(const AttnParams &p, int b) {
     const bool ok = !(u.i0 < 0 || i1 < u.i0 || i1 > p.M || i1 - u.i0 > p.max_nodes);
     u.n = ok ? (int)(i1 - u.i0) : 0;
     const int64_t room = (int64_t)p.max_pages * p.paging.page;
-    u.len = min(max(len, 0), (int)min(room, (int64_t)INT32_MAX));
+    u.len = min(max(len, 0), (int)min(room, kMostSlots));
     u.cache_tiles = paged_tiles(p.paging, u.len);
     u.q_items = (u.n + 2 * p.npt - 1) / (2 * p.npt);
     return u;
@@ -889,6 +889,13 @@ __global__ void __launch_bounds__(kJoinThreads) tree_attention_join(const __grid
 template <typename T, int D, bool kCap>
 int launch(const AttnParams &p, int grid, cudaStream_t stream) {
     auto kernel = tree_attention<T, D, kCap>;
+    // The softmax threads' registers come from what the others give back, and setmaxnreg waits until there are enough:
+    // with fewer than 168 a thread at launch that would be for good.
+    static const bool enough = [&] {
+        cudaFuncAttributes a;
+        return cudaFuncGetAttributes(&a, kernel) == cudaSuccess && a.numRegs >= kLaunchRegisters;
+    }();
+    if (!enough) { record_cuda_error(cudaErrorInvalidDeviceFunction); return SSD_ERR_CUDA; }
     cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void *>(kernel), Shape<D>::kBytes);
     if (e == cudaSuccess) e = launch_pdl(kernel, (unsigned)grid, kWarps * 32u, (size_t)Shape<D>::kBytes, stream, p);
     if (e == cudaSuccess)

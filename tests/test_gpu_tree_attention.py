@@ -205,3 +205,73 @@ def test_captured_and_on_two_streams(cuda_device):
     torch.cuda.synchronize()
     c.lens[0] = 77
     check(c, out)
+
+
+def test_one_long_cache_cut_into_as_many_parts_as_there_are(cuda_device):
+    """One kv head and one utterance: every CTA has a part of the same item."""
+    c = Case(30, [2], [40_001], Hq=2, Hkv=1, page=64, dtype=torch.float16).spoil_unused()
+    check(c, run(c, cuda_device))
+
+
+def test_more_utterances_than_costs_are_held_for(cuda_device):
+    rng = np.random.default_rng(31)
+    B = 4500                                                      # 4,096 are held in front of the walk where heads have 64 values
+    c = Case(31, rng.integers(0, 3, B), rng.integers(0, 20, B), Hq=2, Hkv=1, page=8)
+    r = run(c, cuda_device)
+    check(c, r)
+    assert (r["utt_status"] == 0).all()
+
+
+@pytest.mark.parametrize("cap", [1e-30, 1e-3, 1.0, 1e6])
+def test_caps_of_any_size(cuda_device, cap):
+    c = Case(32, [9, 40], [200, 70], spread=10.0).spoil_unused()
+    check(c, run(c, cuda_device, cap=cap), cap=cap)
+
+
+@pytest.mark.parametrize("scale", [1e-20, 1e-3, 1.0])
+def test_scales_of_any_size(cuda_device, scale):
+    c = Case(33, [9, 40], [200, 70], spread=1.0 if scale < 1 else 0.25).spoil_unused()
+    c.scale = scale
+    check(c, run(c, cuda_device))
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_random_batches(cuda_device, seed):
+    rng = np.random.default_rng(100 + seed)
+    B, Hkv = int(rng.integers(1, 9)), int(rng.integers(1, 5))
+    chain = bool(rng.random() < 0.4)
+    top = int(rng.choice([1, 4, 40, 140]))
+    c = Case(200 + seed, rng.integers(0, top + 1, B), rng.integers(0, int(rng.choice([2, 130, 700])), B), Hq=Hkv * int(rng.choice([1, 2, 3, 4, 8])),
+             Hkv=Hkv, D=int(rng.choice([64, 128])), page=int(rng.choice([1, 5, 8, 16, 40, 64, 128, 160])),
+             dtype=torch.bfloat16 if rng.random() < 0.5 else torch.float16, chain=chain, roots=1 if chain else int(rng.integers(1, 4))).spoil_unused()
+    cap = float(rng.choice([0.0, 0.0, 10.0]))
+    r = run(c, cuda_device, cap=cap)
+    check(c, r, cap=cap)
+    again = run(c, cuda_device, cap=cap)
+    assert torch.equal(r["out"], again["out"]) and torch.equal(r["lse"], again["lse"])
+
+
+def test_rows_behind_the_last_utterance_are_left_alone(cuda_device):
+    c = Case(34, [5, 6], [30, 40])
+    d = c.on(cuda_device)
+    more = lambda x: torch.cat([x, torch.full_like(x[:7], float("nan"))])  # noqa: E731
+    e = dict(d, q=more(d["q"]), tk=more(d["tk"]), tv=more(d["tv"]), parent=torch.cat([d["parent"], d["parent"][:7]]))
+    out = ssd.alloc_tree_attention_outputs(c.M + 7, c.B, c.Hq, c.D, c.dtype, cuda_device)
+    out["out"].fill_(5.0)
+    out["lse"].fill_(6.0)
+    r = run(c, cuda_device, d=e, out=out)
+    check(c, dict(out=r["out"][:c.M], lse=r["lse"][:c.M]))
+    assert (r["out"][c.M:] == 5.0).all() and (r["lse"][c.M:] == 6.0).all()
+
+
+def test_without_lse_and_a_workspace_left_over(cuda_device):
+    c = Case(35, [12, 3], [900, 500], Hq=4, Hkv=1)
+    want = run(c, cuda_device)["out"]
+    out = ssd.alloc_tree_attention_outputs(c.M, c.B, c.Hq, c.D, c.dtype, cuda_device, 1, c.max_nodes)
+    out["workspace"].fill_(255)
+    del out["lse"]
+    assert torch.equal(run(c, cuda_device, out=out)["out"], want)
+    out["workspace"] = out["workspace"][:256]
+    with pytest.raises(ssd.SsdError) as e:
+        run(c, cuda_device, out=out)
+    assert e.value.code == ssd.ERR_WORKSPACE
