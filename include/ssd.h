@@ -6,7 +6,9 @@
  *     log-sum-exp, entropy and greedy argmax; the collapsed draft hypothesis; the
  *     utterance-level entropy gate;
  *   stage 2 (ssd_verify): from the LLM's logits at the draft positions, each draft token's
- *     log-likelihood, the relaxed acceptance rule and the accepted prefix length.
+ *     log-likelihood, the relaxed acceptance rule and the accepted prefix length;
+ *   draft trees (ssd_tree_attention, ssd_verify_tree, ssd_cache_*): drafts that branch, and the
+ *     key/value cache that the LLM's pass over them reads, grows and gives up slots of.
  *
  * Conventions for every call
  *   - All array pointers are DEVICE pointers owned by the caller unless a comment says
@@ -49,10 +51,11 @@ enum {
     SSD_OK = 0,
     SSD_ERR_NULL = 1,      /* a required pointer is NULL */
     SSD_ERR_ARG = 2,       /* negative size, ld < V, blank_id outside [0,V), bad option ... */
-    SSD_ERR_DTYPE = 3,     /* dtype is neither SSD_F32 nor SSD_BF16 */
+    SSD_ERR_DTYPE = 3,     /* a dtype that the call does not take */
     SSD_ERR_WORKSPACE = 4, /* workspace NULL or smaller than the *_workspace_bytes() answer */
     SSD_ERR_CUDA = 5,      /* a CUDA runtime call failed; see ssd_last_cuda_error() */
-    SSD_ERR_ALIGN = 6,     /* logits base not aligned to the element size */
+    SSD_ERR_ALIGN = 6,     /* logits base not aligned to the element size; an address or a stride of a cache,
+                              of queries, keys, values or outputs not a multiple of 16 bytes */
     SSD_ERR_TOO_LARGE = 7  /* ssd_verify_static: the sizes need more scratch than its fixed array */
 };
 

@@ -97,10 +97,10 @@ const char *ssd_status_string(int32_t status) {
         case SSD_OK: return "SSD_OK";
         case SSD_ERR_NULL: return "SSD_ERR_NULL: a required pointer is NULL";
         case SSD_ERR_ARG: return "SSD_ERR_ARG: invalid size, leading dimension, id or option";
-        case SSD_ERR_DTYPE: return "SSD_ERR_DTYPE: dtype must be SSD_F32 or SSD_BF16";
+        case SSD_ERR_DTYPE: return "SSD_ERR_DTYPE: a dtype that the call does not take (logits: SSD_F32, SSD_BF16; caches: SSD_BF16, SSD_F16)";
         case SSD_ERR_WORKSPACE: return "SSD_ERR_WORKSPACE: workspace missing, misaligned or too small";
         case SSD_ERR_CUDA: return "SSD_ERR_CUDA: a CUDA runtime call failed";
-        case SSD_ERR_ALIGN: return "SSD_ERR_ALIGN: logits not aligned to the element size";
+        case SSD_ERR_ALIGN: return "SSD_ERR_ALIGN: logits not aligned to the element size, or a cache's array not to 16 bytes";
         case SSD_ERR_TOO_LARGE:
             return "SSD_ERR_TOO_LARGE: the sizes need more scratch than ssd_verify_static's fixed array";
         default: return "unknown status";

