@@ -275,3 +275,18 @@ def test_without_lse_and_a_workspace_left_over(cuda_device):
     with pytest.raises(ssd.SsdError) as e:
         run(c, cuda_device, out=out)
     assert e.value.code == ssd.ERR_WORKSPACE
+
+
+@pytest.mark.parametrize("cap", [0.0, 20.0])
+@pytest.mark.parametrize("n,lens", [([6, 5], [20, 0]), ([140, 5], [20, 300]), ([6], [3000])])
+def test_a_query_of_nan_stays_its_own(cuda_device, cap, n, lens):
+    """The rows of a tile share their accumulators and their warps' choices: one head of one node is NaN, it alone is in
+    the results, and everything else is right."""
+    c = Case(36, n, lens).spoil_unused()
+    d = c.on(cuda_device)
+    d["q"][2, 1, 3] = float("nan")
+    r = run(c, cuda_device, cap=cap, d=d)
+    assert torch.isnan(r["out"][2, 1].float()).all() and torch.isnan(r["lse"][2, 1])
+    whole = run(c, cuda_device, cap=cap)
+    r["out"][2, 1], r["lse"][2, 1] = whole["out"][2, 1], whole["lse"][2, 1]
+    check(c, r, cap)
