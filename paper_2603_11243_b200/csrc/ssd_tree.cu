@@ -72,8 +72,8 @@ template <int D> struct Shape {
     static constexpr int kSlots = D == 128 ? 5 : 8;
     static constexpr int kRing = 2 * kSlotBytes;                  // behind the two tiles of queries
     static constexpr int kMisc = kRing + kSlots * kSlotBytes;
-    static constexpr int kBars = kMisc;     // full[], empty[], q full[2], q empty[2], scores[2], probs[2], sums[2], sums free
-    static constexpr int kNumBars = 2 * kSlots + 16;              // and segments full[2], empty[2], softmax warps together
+    static constexpr int kBars = kMisc;     // full[], empty[], q full[2], q empty[2], scores[2], probs[2], sums[2], sums free[2]
+    static constexpr int kNumBars = 2 * kSlots + 17;              // and segments full[2], empty[2], softmax warps together
     static constexpr int kWords = kBars + kNumBars * 8;           // tmem address, failed, bad value seen [2]
     static constexpr int kMl = (kWords + 16 + 15) / 16 * 16;      // [2][128] running maximum and sum
     static constexpr int kParent = kMl + 2 * kTile * 8;
@@ -342,10 +342,10 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
     auto scores_full = [&](int s) { return more + 32 + 8 * s; };
     auto probs_ready = [&](int s) { return more + 48 + 8 * s; };
     auto sums_full = [&](int s) { return more + 64 + 8 * s; };
-    const uint32_t sums_free = more + 80;
-    auto segment_full = [&](int i) { return more + 88 + 8 * i; };
-    auto segment_empty = [&](int i) { return more + 104 + 8 * i; };
-    const uint32_t together = more + 120;
+    auto sums_free = [&](int s) { return more + 80 + 8 * s; };
+    auto segment_full = [&](int i) { return more + 96 + 8 * i; };
+    auto segment_empty = [&](int i) { return more + 112 + 8 * i; };
+    const uint32_t together = more + 128;
     volatile Segment *const ring = reinterpret_cast<volatile Segment *>(base + S::kSegments);
     volatile uint32_t *const words = reinterpret_cast<volatile uint32_t *>(base + S::kWords);
     volatile uint32_t *const failed = words + 1;
@@ -362,11 +362,11 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
             mbar_init(q_empty(s), 1);
             mbar_init(scores_full(s), 1);
             mbar_init(probs_ready(s), 4);
+            mbar_init(sums_free(s), 8);
             mbar_init(sums_full(s), 1);
             mbar_init(segment_full(s), 1);
             mbar_init(segment_empty(s), 11);
         }
-        mbar_init(sums_free, 8);
         mbar_init(together, 8);
         mbar_init_fence();
         words[1] = words[2] = words[3] = 0;
@@ -496,7 +496,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
                 auto values = [&](int u, int n16) {
                     const int s = u & 1, k = u >> 1, tile = pair ? k : u, pos = pos0 + 2 * tile + 1;
                     ok = ok && mbar_wait_bounded(slot_full(pos % S::kSlots), (pos / S::kSlots) & 1);
-                    if (u == 0 && g > 0) ok = ok && mbar_wait_bounded(sums_free, (g - 1) & 1);
+                    if (k == 0 && g > 0) ok = ok && mbar_wait_bounded(sums_free(s), (g - 1) & 1);
                     ok = ok && mbar_wait_bounded(probs_ready(s), (done[s] + k) & 1);
                     if (!ok) return;
                     tc_fence_after();
@@ -534,6 +534,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
                 if (!ok) break;
                 if (lane == 0) {
                     volatile Segment &n = ring[g & 1];
+                    words[2 + (g & 1)] = 0;                       // nobody reads the earlier item's any more
                     n.i0 = k.u.i0;
                     n.b = k.b; n.h = k.h; n.n = k.u.n; n.len = k.u.len;
                     n.node0 = k.it.node0; n.pair = k.it.pair; n.last = k.it.last; n.tree_tiles = k.it.tree_tiles; n.tiles = k.it.tiles;
@@ -612,6 +613,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
             line = __shfl_sync(0xffffffffu, mask, node & 31);
         }
         if (p.parent && !small && begin < w.tree_tiles) {
+            meet();                                  // the earlier item's are read
             for (int j = tid; j < min(w.last, kParents); j += 256) {
                 const int up = p.parent[w.i0 + j];
                 parents[j] = (int16_t)(up < -1 || up >= j ? -1 : up);
@@ -733,7 +735,9 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
         done += count;
         pos0 += 2 * tiles;
         // ---- what came of it ------------------------------------------------------------------------
-        ml[s * kTile + row] = make_float2(m, l);
+        // A pair's streams have nothing to do with one another: each ends when it does (chains 484 -> 461 us against a
+        // meeting).  Those of one tile meet.
+        if (!pair) ml[s * kTile + row] = make_float2(m, l);
         const bool any[2] = {true, pair || tiles > 1};                 // whether a stream had tiles
         for (int i = 0; i < 2; ++i)
             if (any[i]) {
@@ -741,7 +745,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
                 ++closed[i];
             }
         if (!ok) *failed = 1;
-        meet();
+        if (!pair) meet();
         tc_fence_after();
         const bool sick = *seen != 0;
         // a pair of tiles: this stream's sums; else the two streams' of one tile, half the columns each
@@ -811,7 +815,10 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(sums_free);
+        if (lane == 0) {                             // eight arrivals: of one stream's warps, or of all
+            mbar_arrive(sums_free(pair ? s : 1));
+            mbar_arrive(sums_free(pair ? s : 0));
+        }
         if (live && (pair || s == 0)) {
             if (!whole) reinterpret_cast<float2 *>(part)[tile_q * tile_rows + row] = make_float2(m, l);
             else if (p.lse) p.lse[(w.i0 + node) * p.Hq + head] = l == 0.f ? -INFINITY : (m * c) * kLn2 + (logf(l) - kLift * kLn2);
@@ -829,8 +836,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
             if (g == 0) cut.first_b = w.b;
             cut.last_b = w.b;
         }
-        meet();                                      // everyone is done with ml, parents and seen
-        if (tid == 0) *seen = 0;
+        if (!pair) meet();                           // everyone is done with ml
     }
     if (!ok) *failed = 1;
     tc_fence_before();

@@ -11,7 +11,7 @@ import pytest
 import torch
 
 from paper_2603_11243_b200 import binding as ssd
-from tree_ref import Case
+from tree_ref import Case, lines
 
 pytestmark = pytest.mark.gpu
 HALF_STEP = {torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
@@ -290,3 +290,26 @@ def test_a_query_of_nan_stays_its_own(cuda_device, cap, n, lens):
     whole = run(c, cuda_device, cap=cap)
     r["out"][2, 1], r["lse"][2, 1] = whole["out"][2, 1], whole["lse"][2, 1]
     check(c, r, cap)
+
+
+@pytest.mark.parametrize("chain", [True, False])
+def test_many_items_of_one_and_of_two_tiles(cuda_device, chain):
+    """Several items to a multiprocessor, of one tile of queries and of two in any order, trees that are walked and trees
+    that are not: what an item leaves in shared memory is not the next one's."""
+    rng = np.random.default_rng(37)
+    n = rng.choice([1, 5, 31, 33, 40, 64, 65, 100, 130], 160)
+    c = Case(37, n, rng.integers(0, 300, 160), Hq=8, Hkv=2, D=64, chain=chain, roots=1 if chain else 3).spoil_unused()
+    d = c.on(cuda_device)
+    clean = run(c, cuda_device, d=d)
+    check(c, clean)
+    off = c.off
+    d["tv"][torch.as_tensor(off[:-1:7], device=cuda_device), 1, 9] = float("nan")       # an utterance's first node
+    r = run(c, cuda_device, d=d)
+    hit = torch.zeros(c.M, dtype=torch.bool)
+    for b in range(0, 160, 7):
+        for i, line in enumerate(lines(c.parent[off[b]:off[b + 1]])):
+            hit[off[b] + i] = 0 in line
+    got, want = r["out"].cpu(), clean["out"].cpu()
+    assert torch.isnan(got[hit][:, 4:, 9]).all()
+    got[hit, 4:, 9] = want[hit, 4:, 9]
+    assert torch.equal(got, want) and torch.equal(r["lse"], clean["lse"])
