@@ -5,7 +5,9 @@
 // holds one key and adds over the columns in its registers, so nothing crosses lanes and every slot has one
 // writer.  A CTA has a tile of 128 slots and goes over the heads, and over tiles of queries within a head;
 // where there are few tiles, the heads are dealt out to a cluster of CTAs whose sums meet in shared memory.  Two
-// groups of four warps take turns at the products' results, warp 8 issues the copies, warp 9 the products.
+// groups of four warps take turns at the products' results, warp 8 issues the copies of queries, warp 10 those of
+// keys, warp 9 the products.  (One warp for both kinds kept keys waiting for queries' slots: 184 us instead of 156
+// on 128 caches of 500 to 3,000 slots, 896 MB.)
 //
 // Measured: trees of 5 to 32 nodes on 32 caches of 500 to 3,000 slots, 16 heads of 128, fp16: 51 us, 224 MB at 4.4 TB/s;
 // one token's weights over 8 caches of up to 2,000 slots: 9.6 us with the host's call.
@@ -18,7 +20,7 @@ namespace {
 
 using namespace tc;
 
-constexpr int kWarps = 10;
+constexpr int kWarps = 11;
 
 struct alignas(64) WeightParams {
     CUtensorMap q, cache_k;
@@ -117,7 +119,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cache_weights(const __grid_con
     pdl_launch_dependents();
     const uint32_t tmem = words[0];
 
-    if (warp == 8) {
+    if (warp == 10) {
         const int page_count = p.paging.pages ? p.paging.pages : 1;
         int id = p.n_pages;                                      // outside: the copy fills in zeros
         if (lane < page_count && at.page + lane < p.max_pages) {
@@ -129,19 +131,18 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cache_weights(const __grid_con
         const int i = lane / S::kBlocks, x = lane % S::kBlocks;
         const int page = __shfl_sync(0xffffffffu, id, p.paging.pages ? i : 0);
         bool ok = true;
-        auto keys = [&](int k) {
-            if (k >= S::kKeySlots) ok = ok && mbar_wait_bounded(keys_empty(k), (k / S::kKeySlots - 1) & 1);
-            if (!ok) return;
+        for (int k = 0; k < heads && ok; ++k) {
+            if (k >= S::kKeySlots) ok = mbar_wait_bounded(keys_empty(k), (k / S::kKeySlots - 1) & 1);
+            if (!ok) break;
             if (lane == 0) mbar_arrive_expect_tx(keys_full(k), copies * box * 128 * S::kBlocks);
             __syncwarp();
             if (i < copies)
                 tma_load_4d(keys_at(k) + x * kBlockBytes + i * box * 128, &p.cache_k, x * 64, rank + k * p.split,
                             p.paging.pages ? 0 : at.slot + i * box, page, keys_full(k));
-        };
-        // Later heads' keys are asked for when the head that had their slot is as good as done: its last queries are
-        // under way, and so are the next head's first.
-        int ahead = 0;
-        for (; ahead < heads && ahead < S::kKeySlots; ++ahead) keys(ahead);
+        }
+        if (!ok) words[1] = 1;
+    } else if (warp == 8) {
+        bool ok = true;
         for (int k = 0, u = 0; k < heads && ok; ++k) {
             for (int c = 0; c < chunks && ok; ++c, ++u) {
                 const int q = u % q_slots;
@@ -151,7 +152,6 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cache_weights(const __grid_con
                 __syncwarp();
                 if (lane < S::kBlocks)
                     tma_load_3d(q_at(q) + lane * q_block, &p.q, lane * 64, (rank + k * p.split) * p.G, (int)i0 + c * p.npt, q_full(q));
-                if (c == 0 && k > 0 && ahead < heads) keys(ahead++);
             }
         }
         if (!ok) words[1] = 1;
