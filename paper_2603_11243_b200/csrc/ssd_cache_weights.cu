@@ -9,8 +9,8 @@
 // keys, warp 9 the products.  (One warp for both kinds kept keys waiting for queries' slots: 184 us instead of 156
 // on 128 caches of 500 to 3,000 slots, 896 MB.)
 //
-// Measured: trees of 5 to 32 nodes on 32 caches of 500 to 3,000 slots, 16 heads of 128, fp16: 51 us, 224 MB at 4.4 TB/s;
-// one token's weights over 8 caches of up to 2,000 slots: 9.6 us with the host's call.
+// Measured: trees of 5 to 32 nodes on 32 caches of 500 to 3,000 slots, 16 heads of 128, fp16: 48 us, 224 MB at 4.6 TB/s;
+// one token's weights over 8 caches of up to 2,000 slots: 8.8 us with the host's call.
 #include <math.h>
 
 #include "ssd_tc.cuh"

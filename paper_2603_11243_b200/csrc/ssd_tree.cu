@@ -20,8 +20,8 @@
 // closing kernel joins.
 //
 // Measured (32 query and 8 kv heads of 128, bf16, pages of 16): trees of 5 to 32 nodes on 64 caches of 500 to
-// 3,000 slots 120 us, 475 MB at 3.9 TB/s; chains of 50 to 200 nodes on 128 caches of 250 to 1,500 slots 502 us, 256 GFLOP at
-// 509 TFLOP/s.  A key tile takes a CTA 2,400 clocks either way: at few rows that is what HBM gives a
+// 3,000 slots 119 us, 475 MB at 4.0 TB/s; chains of 50 to 200 nodes on 128 caches of 250 to 1,500 slots 490 us, 256 GFLOP at
+// 522 TFLOP/s.  A key tile takes a CTA 2,400 clocks either way: at few rows that is what HBM gives a
 // multiprocessor, at many it is the cycle scores -> softmax -> product of a stream (4,500 clocks) over two streams, of
 // which the products are 1,220 and the softmax 2,250.
 #include <math.h>
