@@ -510,7 +510,8 @@ int32_t ssd_cache_append(const ssd_heads *tree_k, const ssd_heads *tree_v, const
  *                                    their heads of exp(s_is - lse[i, head]),       s < len[b]
  * with the scores of ssd_tree_attention, whose lse this takes (use: its on_path counts accepted nodes
  * only).  Sums are fp32 and in a fixed order: the same inputs give the same bits.  Queries and lse of
- * nodes that do not count have no influence, NaN included.  cache->v is not looked at.
+ * nodes that do not count have no influence, NaN included; a NaN in one that counts makes its utterance's
+ * weights NaN.  cache->v is not looked at.
  * Slots from weight_cols on are left out (SSD_UTT_BAD_CACHE where len says there are some).
  * Errors: as ssd_tree_attention.
  */

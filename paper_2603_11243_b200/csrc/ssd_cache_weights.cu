@@ -11,6 +11,7 @@
 //
 // Measured: trees of 5 to 32 nodes on 32 caches of 500 to 3,000 slots, 16 heads of 128, fp16: 48 us, 224 MB at 4.6 TB/s;
 // one token's weights over 8 caches of up to 2,000 slots: 8.8 us with the host's call.
+#include <float.h>
 #include <math.h>
 
 #include "ssd_tc.cuh"
@@ -195,7 +196,10 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cache_weights(const __grid_con
                 for (int r = lane; r < (rows + 15) / 16 * 16; r += 32) {
                     float x = INFINITY;                          // not counted: the probability is 0
                     const int64_t node = i0 + chunk * p.npt + r / p.G;
-                    if (r < rows && (!p.use || p.use[node])) x = p.lse[node * p.Hq + h * p.G + r % p.G] * kLog2e;
+                    if (r < rows && (!p.use || p.use[node])) {
+                        x = p.lse[node * p.Hq + h * p.G + r % p.G] * kLog2e;
+                        if (x == INFINITY) x = FLT_MAX;          // a counted row's infinity: 0 all the same, but for a score of NaN
+                    }
                     lse[r] = x;
                 }
                 __syncwarp();
@@ -221,7 +225,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) cache_weights(const __grid_con
                         a[0] = a[1] = a[2] = a[3] = 0.f;         // (added in the same order: the same bits without it)
 #pragma unroll
                         for (int i = 0; i < 32; ++i)
-                            if (i < 16 || !half) a[i & 3] += lse[j + i] < INFINITY ? x[i] : 0.f;
+                            if (i < 16 || !half) a[i & 3] += lse[j + i] == INFINITY ? 0.f : x[i];
                         more = (a[0] + a[1]) + (a[2] + a[3]);
                     }
                     sum += more;

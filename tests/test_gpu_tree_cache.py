@@ -306,3 +306,36 @@ def test_a_verification_pass_over_trees(cuda_device):
     ssd.ssd_tree_attention(d["q"], d["tk"], d["tv"], d["k"], d["v"], d["table"], evi["new_len"], d["off"], c.max_nodes, d["parent"], out=att)
     out, _ = c.attention()
     assert ((att["out"].cpu().double() - out).norm() / out.norm()) < 5e-3
+
+
+@pytest.mark.parametrize("what", ["lse", "query", "both"])
+def test_weights_of_a_counted_node_that_is_nan(cuda_device, what):
+    """exp(s - lse) of a counted node is NaN where either is: its utterance's slots become NaN (never a sum without it),
+    the other utterance's do not."""
+    c = Case(40, [7, 40], [300, 150])
+    lse = c.attention()[1].float()
+    use = torch.ones(c.M, dtype=torch.uint8)
+    use[[2, 9]] = 0
+    want, _ = run_weights(c, cuda_device, lse, use)
+    if what != "lse":
+        c.q[4, 3, 5] = math.nan
+    if what != "query":
+        lse[4, 3] = math.nan
+    got, _ = run_weights(c, cuda_device, lse, use)
+    assert torch.isnan(got[0, :300]).all()
+    assert torch.equal(got[1, :150], want[1, :150])
+
+
+def test_weights_of_a_counted_node_with_an_infinite_lse(cuda_device):
+    """exp(s - inf) is 0 for a score s, and NaN for one that is NaN: only use == 0 takes a node out."""
+    c = Case(41, [7, 40], [300, 150])
+    lse = c.attention()[1].float()
+    use = torch.ones(c.M, dtype=torch.uint8)
+    use[4] = 0
+    without, _ = run_weights(c, cuda_device, lse, use)
+    lse[4] = math.inf
+    got, _ = run_weights(c, cuda_device, lse)
+    assert torch.equal(got, without)
+    c.q[4, 3, 5] = math.nan
+    got, _ = run_weights(c, cuda_device, lse)
+    assert torch.isnan(got[0, :300]).all() and torch.equal(got[1, :150], without[1, :150])
