@@ -278,6 +278,7 @@ int launch_cache_weights(const ssd_heads &q, const float *lse, const ssd_kv_cach
                          int64_t M, int max_nodes, float scale, float cap, const uint8_t *use, float *weight,
                          int64_t weight_stride, int weight_cols, uint32_t *status, cudaStream_t stream) {
     if (B == 0) return SSD_OK;
+    cap = tc::cap_in_range(scale, cap);
     WeightParams p;
     p.paging = paging(cache.page_size);
     p.G = q.heads / cache.heads;

@@ -10,6 +10,7 @@
 #pragma once
 
 #include <cuda.h>
+#include <float.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -163,7 +164,7 @@ template <> __device__ __forceinline__ uint32_t pack2<__half>(float lo, float hi
 // at least 0.46.
 // `counts`: whether the thread's scores are anybody's (what lies in other rows must not send a warp the long way).
 template <int N> __device__ __forceinline__ void cap_scores(float *x, float scale, float cap, bool counts) {
-    const float r = scale / cap;
+    const float r = fminf(scale / cap, FLT_MAX);         // of a cap of no size: a score of 0 stays 0, others become the cap
     constexpr float c1 = -0.33333069394019127f, c2 = 0.13324779317551644f, c3 = -0.05298607528769192f, c4 = 0.01713500662684319f;
     float top[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -199,6 +200,9 @@ template <int N> __device__ __forceinline__ void cap_scores(float *x, float scal
         }
     }
 }
+// The cap that the kernels take.  Where scale / cap lies below fp32's normal numbers it would lose digits, and the cap
+// changes nothing: cap tanh(s / cap) is s but for (s / cap)^2 / 3 of it, 5e-9 for a product of query and key of 1e34.
+inline float cap_in_range(float scale, float cap) { return cap > 0.f && scale / cap < FLT_MIN ? 0.f : cap; }
 // where the 16-byte unit `unit` of row `row` of a tile lies
 __device__ __forceinline__ uint32_t unit_at(uint32_t tile, int row, int unit) {
     return tile + (unit >> 3) * kBlockBytes + row * 128 + (((unit & 7) ^ (row & 7)) << 4);

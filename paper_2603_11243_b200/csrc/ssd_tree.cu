@@ -991,6 +991,7 @@ int launch_tree_attention(const ssd_heads &q, const ssd_heads &tree_k, const ssd
                           const int64_t *tok_off, const int32_t *parent, int B, int64_t M, int max_nodes, float scale,
                           float cap, const ssd_heads &out, float *lse, uint32_t *status, void *workspace, cudaStream_t stream) {
     if (B == 0) return SSD_OK;
+    cap = tc::cap_in_range(scale, cap);
     const int sms = device_sm_count();
     if (sms <= 0) return SSD_ERR_CUDA;
     AttnParams p;

@@ -313,3 +313,26 @@ def test_many_items_of_one_and_of_two_tiles(cuda_device, chain):
     assert torch.isnan(got[hit][:, 4:, 9]).all()
     got[hit, 4:, 9] = want[hit, 4:, 9]
     assert torch.equal(got, want) and torch.equal(r["lse"], clean["lse"])
+
+
+@pytest.mark.parametrize("cap", [1e-45, 1e-40, 1e37, 3e38])
+def test_caps_whose_ratio_to_the_scale_is_no_normal_number(cuda_device, cap):
+    """scale / cap leaves fp32's range: scores of 0 stay 0 (not 0 * inf), and a cap far above every score changes none."""
+    c = Case(42, [9, 40], [200, 70], spread=10.0).spoil_unused()
+    c.q[3] = 0
+    check(c, run(c, cuda_device, cap=cap), cap=cap)
+
+
+def test_broadcast_heads_and_rows(cuda_device):
+    """Strides of 0: one kv head for all (keys, values and cache), one row of queries for every node."""
+    c = Case(43, [9, 40], [200, 70], Hq=8, Hkv=2)
+    for name in ("k", "v", "tk", "tv"):
+        x = getattr(c, name)
+        x[..., 1, :] = x[..., 0, :]
+    c.q[:] = c.q[:1].clone()
+    d = c.on(cuda_device)
+    for name in ("k", "v", "tk", "tv"):
+        d[name] = d[name][..., :1, :].contiguous().expand(d[name].shape)
+    d["q"] = d["q"][:1].contiguous().expand(d["q"].shape)
+    assert d["tk"].stride(1) == 0 and d["k"].stride(2) == 0 and d["q"].stride(0) == 0
+    check(c, run(c, cuda_device, d=d))

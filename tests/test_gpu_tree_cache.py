@@ -339,3 +339,13 @@ def test_weights_of_a_counted_node_with_an_infinite_lse(cuda_device):
     c.q[4, 3, 5] = math.nan
     got, _ = run_weights(c, cuda_device, lse)
     assert torch.isnan(got[0, :300]).all() and torch.equal(got[1, :150], without[1, :150])
+
+
+@pytest.mark.parametrize("cap", [1e-45, 1e-40, 1e37, 3e38])
+def test_weights_at_caps_whose_ratio_to_the_scale_is_no_normal_number(cuda_device, cap):
+    c = Case(44, [9, 40], [200, 70]).spoil_unused()
+    c.q[3] = 0
+    lse = c.attention(cap)[1].float()
+    got, status = run_weights(c, cuda_device, lse, cap=cap)
+    want = weights(c, lse, None, cap)
+    assert ((got.cpu().double() - want).abs() <= 1e-5 * want + 1e-12).all() and not status.any()
