@@ -474,6 +474,7 @@ int32_t ssd_tree_attention(const ssd_heads *q, const ssd_heads *tree_k, const ss
  * Auto-regressive decoding resumes from the logits of the path's last node.  A parent out of range
  * makes its node rejected (SSD_UTT_BAD_PARENT).  skip [B] u8 (nullable): nonzero = not verified: the
  * rows are not read, path_len = 0, token_logp and row_lse untouched.  Malformed offsets: path_len = 0.
+ * Where two utterances' offsets name the same rows, what is written for those rows is unspecified.
  * logits [M, ld] dtype, read once; draft_ids, parent, path [M] i32; token_logp, row_lse [M] f32;
  * on_path [M] u8; path_len [B] i32; utt_status [B] u32.
  * workspace: as ssd_verify (ssd_verify_workspace_bytes(B, M, V, dtype, opts)).

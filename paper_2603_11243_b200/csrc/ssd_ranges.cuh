@@ -30,6 +30,22 @@ SSD_HD int64_t row_of_utterance(int64_t i0, int64_t i1, int64_t M, int k) {
     return rows_sound(i0, i1, M) && k < i1 - i0 ? i0 + k : -1;
 }
 
+// The accepted path of a draft tree of n nodes, from its last node upwards: `depth` entries of path, and their marks.
+// Returns the path's length.  Depths, nodes and parents may be anything: utterances that name the same rows, as
+// offsets may, overwrite each other's, and no entry outside of this one's may come of it.
+template <typename Up>
+SSD_HD int write_path(int32_t *path, uint8_t *on_path, int n, int node, int depth, Up up_of) {
+    const int length = depth < n ? (depth > 0 ? depth : 0) : n;
+    int j = node;
+    for (int k = length - 1; k >= 0 && j >= 0 && j < n; --k) {
+        path[k] = j;
+        on_path[j] = 1;
+        const int up = up_of(j);
+        j = up < j ? up : -1;
+    }
+    return length;
+}
+
 // ---- frame statistics: one tile = R consecutive rows, fetched as one contiguous range --------
 // The tile's bytes are [gstart, gend).  Its 16-byte-aligned superset [f0, c1) is what lands in
 // the stage (stage byte 0 holds address f0).  Where that superset would leave the matrix

@@ -845,13 +845,8 @@ __global__ void __launch_bounds__(kFinishThreads) tree_finish_kernel(
     for (int i = tid; i < n; i += blockDim.x) { path[i0 + i] = -1; on_path[i0 + i] = 0; }
     __syncthreads();
     if (tid == 0) {
-        int j = best_node;
-        for (int k = best_depth - 1; k >= 0; --k) {
-            path[i0 + k] = j;
-            on_path[i0 + j] = 1;
-            j = shared ? s_up[j] : parent ? parent[i0 + j] : j - 1;
-        }
-        path_len[b] = best_depth;
+        path_len[b] = ranges::write_path(path + i0, on_path + i0, n, best_node, best_depth,
+                                         [&](int j) { return shared ? s_up[j] : parent ? parent[i0 + j] : j - 1; });
         utt_status[b] = flags | internal;
     }
 }

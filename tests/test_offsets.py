@@ -18,6 +18,9 @@ SOURCE = """
 extern "C" long long row(long long i0, long long i1, long long M, int k) {
     return ssd::ranges::row_of_utterance(i0, i1, M, k);
 }
+extern "C" int path(int *p, unsigned char *on, int n, int node, int depth, const int *parent) {
+    return ssd::ranges::write_path(p, on, n, node, depth, [&](int j) { return parent[j]; });
+}
 extern "C" int sound(long long i0, long long i1, long long M) { return ssd::ranges::rows_sound(i0, i1, M); }
 """
 
@@ -69,3 +72,47 @@ def test_offsets_at_the_ends_of_int64(cuda_device, kernel):
         assert H.status_u32(out["utt_status"]).tolist() == [ssd.UTT_BAD_OFFSETS * b for b in bad]
         assert out["accepted_len"].tolist() == lens
         assert out["all_accepted"].tolist() == [1 - b for b in bad]
+
+
+def test_a_path_stays_inside_its_utterance(host):
+    """Whatever a tree's closing kernel is left with where utterances name the same rows: depths above the number of
+    nodes, parents out of range, nodes that are none."""
+    wild = [-(1 << 31), -7, -1, 0, 1, 2, 3, 4, 5, 6, 900, (1 << 31) - 1]
+    guard = 16
+    for n, node, depth in itertools.product((0, 1, 5), wild, wild):
+        for up in wild:
+            parents = (C.c_int * (n + 2 * guard))(*[up] * (n + 2 * guard))
+            p, on = (C.c_int * (n + 2 * guard))(*[77] * (n + 2 * guard)), (C.c_ubyte * (n + 2 * guard))(*[77] * (n + 2 * guard))
+            at = lambda a, size: C.byref(a, guard * size)  # noqa: E731
+            length = host.path(at(p, 4), at(on, 1), n, node, depth, at(parents, 4))
+            assert 0 <= length <= n
+            for a in (p, on):
+                assert list(a[:guard]) == [77] * guard and list(a[guard + n:]) == [77] * guard
+    parents = (C.c_int * 6)(-1, 0, 0, 2, 1, 3)
+    p, on = (C.c_int * 6)(*[-1] * 6), (C.c_ubyte * 6)()
+    assert host.path(p, on, 6, 5, 4, parents) == 4 and list(p) == [0, 2, 3, 5, -1, -1] and list(on) == [1, 0, 1, 1, 0, 1]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("chain", [True, False])
+def test_trees_of_utterances_that_name_the_same_rows(cuda_device, chain):
+    """More nodes than are held in shared memory, so that the two utterances overwrite each other's depths: lengths and
+    entries stay in range, and nothing beside the rows is touched."""
+    V, n, dev = 40, 3000, cuda_device
+    off = torch.tensor([0, 2400, 300, n], dtype=torch.int64, device=dev)      # [0, 2400), malformed, [300, 3000)
+    g = torch.Generator().manual_seed(12)
+    x = torch.randn((n, V), generator=g).to(dev)
+    ids = x.argmax(1).to(torch.int32)
+    parent = None if chain else (torch.arange(n, dtype=torch.int32, device=dev) - 1) // 3 - 120
+    wide = {k: torch.full((n + 512,), 77, dtype=t, device=dev) for k, t in (("path", torch.int32), ("on_path", torch.uint8))}
+    out = ssd.alloc_verify_tree_outputs(n, 3, dev, ssd.ssd_verify_workspace_bytes(3, n, V, ssd.F32))
+    for k in wide:
+        out[k] = wide[k][256:256 + n]
+    for _ in range(20):
+        ssd.ssd_verify_tree(x, off, ids, parent, 0.0, out=out)
+    torch.cuda.synchronize()
+    length = out["path_len"].tolist()
+    assert 0 <= length[0] <= 2400 and length[1] == 0 and 0 <= length[2] <= 2700
+    assert out["path"].min() >= -1 and out["path"].max() < 2700 and out["on_path"].max() <= 1
+    for w in wide.values():
+        assert (w[:256] == 77).all() and (w[256 + n:] == 77).all()
