@@ -46,6 +46,12 @@ SSD_HD int write_path(int32_t *path, uint8_t *on_path, int n, int node, int dept
     return length;
 }
 
+// A CTA of the tree attention's line whose wait has run out knows neither what it has left unwritten nor whose results
+// it was to be joined with: every utterance of the call is told.  By `step` threads, of which this is number `first`.
+SSD_HD void tell_all(uint32_t *status, int B, uint32_t bits, int first, int step) {
+    for (int64_t b = first; b < B; b += step) status[b] = bits;
+}
+
 // ---- frame statistics: one tile = R consecutive rows, fetched as one contiguous range --------
 // The tile's bytes are [gstart, gend).  Its 16-byte-aligned superset [f0, c1) is what lands in
 // the stage (stage byte 0 holds address f0).  Where that superset would leave the matrix

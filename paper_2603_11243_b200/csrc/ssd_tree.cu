@@ -26,6 +26,7 @@
 // which the products are 1,220 and the softmax 2,250.
 #include <math.h>
 
+#include "ssd_ranges.cuh"
 #include "ssd_tc.cuh"
 
 namespace ssd {
@@ -43,7 +44,7 @@ struct Cut {
     int32_t head;                        // 0: none; 1: goes on; 2: ends here
     int32_t tail;                        // 1: there is one
     int32_t b, h, node0, rows;           // the tail's item
-    int32_t first_b, last_b, failed;     // utterances this CTA worked on; whether a wait of its ran out
+    int32_t failed;                      // whether a wait of its ran out
 };
 
 struct alignas(64) AttnParams {
@@ -569,12 +570,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
     const int tile_rows = p.npt * p.G;
     bool ok = true;
     int pos0 = 0, done = 0, closed[2] = {0, 0};
-    if (tid == 0) {
-        Cut none{};
-        none.first_b = 0x7fffffff;
-        none.last_b = -1;
-        p.cuts[blockIdx.x] = none;
-    }
+    if (tid == 0) p.cuts[blockIdx.x] = Cut{};
     // The eight softmax warps wait for one another, with a limit as every wait here: a warp that has given up
     // keeps nobody.
     int meetings = 0;
@@ -823,18 +819,14 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
             if (!whole) reinterpret_cast<float2 *>(part)[tile_q * tile_rows + row] = make_float2(m, l);
             else if (p.lse) p.lse[(w.i0 + node) * p.Hq + head] = l == 0.f ? -INFINITY : (m * c) * kLn2 + (logf(l) - kLift * kLn2);
         }
-        if (tid == 0) {                              // nobody reads these in this grid
+        if (tid == 0 && !whole) {                    // nobody reads these in this grid
             Cut &cut = p.cuts[blockIdx.x];
-            if (!whole) {
-                if (begin > 0) cut.head = w.end == w.tiles ? 2 : 1;
-                else {
-                    cut.tail = 1;
-                    cut.b = w.b; cut.h = w.h; cut.node0 = w.node0;
-                    cut.rows = min((1 + pair) * p.npt, w.n - w.node0) * p.G;
-                }
+            if (begin > 0) cut.head = w.end == w.tiles ? 2 : 1;
+            else {
+                cut.tail = 1;
+                cut.b = w.b; cut.h = w.h; cut.node0 = w.node0;
+                cut.rows = min((1 + pair) * p.npt, w.n - w.node0) * p.G;
             }
-            if (g == 0) cut.first_b = w.b;
-            cut.last_b = w.b;
         }
         if (!pair) meet();                           // everyone is done with ml
     }
@@ -853,8 +845,7 @@ __global__ void __launch_bounds__(kJoinThreads) tree_attention_join(const __grid
     pdl_enter();
     const int first = blockIdx.x / kJoinBlocks, slice = blockIdx.x % kJoinBlocks;
     const Cut cut = p.cuts[first];
-    if (cut.failed && slice == 0)
-        for (int b = cut.first_b + threadIdx.x; b <= cut.last_b; b += kJoinThreads) p.status[b] = SSD_UTT_INTERNAL;
+    if (cut.failed && slice == 0) ranges::tell_all(p.status, p.B, SSD_UTT_INTERNAL, threadIdx.x, kJoinThreads);
     if (!cut.tail || slice * kJoinThreads >= cut.rows * (D / 4)) return;
     const float c = kCap ? kLog2e : p.scale * kLog2e;
     const int64_t stride = 2 * part_floats(p.part_rows, D);

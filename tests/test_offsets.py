@@ -21,6 +21,9 @@ extern "C" long long row(long long i0, long long i1, long long M, int k) {
 extern "C" int path(int *p, unsigned char *on, int n, int node, int depth, const int *parent) {
     return ssd::ranges::write_path(p, on, n, node, depth, [&](int j) { return parent[j]; });
 }
+extern "C" void tell(unsigned *status, int B, unsigned bits, int first, int step) {
+    ssd::ranges::tell_all(status, B, bits, first, step);
+}
 extern "C" int sound(long long i0, long long i1, long long M) { return ssd::ranges::rows_sound(i0, i1, M); }
 """
 
@@ -91,6 +94,17 @@ def test_a_path_stays_inside_its_utterance(host):
     parents = (C.c_int * 6)(-1, 0, 0, 2, 1, 3)
     p, on = (C.c_int * 6)(*[-1] * 6), (C.c_ubyte * 6)()
     assert host.path(p, on, 6, 5, 4, parents) == 4 and list(p) == [0, 2, 3, 5, -1, -1] and list(on) == [1, 0, 1, 1, 0, 1]
+
+
+def test_every_utterance_is_told_that_a_wait_ran_out(host):
+    """Those that the failing CTA never began among them."""
+    for B in (0, 1, 255, 256, 257, 4500):
+        status = (C.c_uint * (B + 300))(*[5] * (B + 300))
+        for thread in range(256):
+            host.tell(status, B, C.c_uint(ssd.UTT_INTERNAL), thread, 256)
+        assert list(status) == [ssd.UTT_INTERNAL] * B + [5] * 300
+    source = open(os.path.join(ROOT, "paper_2603_11243_b200", "csrc", "ssd_tree.cu")).read()
+    assert "if (cut.failed && slice == 0) ranges::tell_all(p.status, p.B, SSD_UTT_INTERNAL," in source
 
 
 @pytest.mark.gpu
