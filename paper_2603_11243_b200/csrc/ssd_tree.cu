@@ -26,6 +26,8 @@
 // which the products are 1,220 and the softmax 2,250.
 #include <math.h>
 
+#include <atomic>
+
 #include "ssd_ranges.cuh"
 #include "ssd_tc.cuh"
 
@@ -896,13 +898,17 @@ template <typename T, int D, bool kCap>
 int launch(const AttnParams &p, int grid, cudaStream_t stream) {
     auto kernel = tree_attention<T, D, kCap>;
     // The softmax threads' registers come from what the others give back, and setmaxnreg waits until there are enough:
-    // with fewer than 168 a thread at launch that would be for good.
-    static const bool enough = [&] {
+    // with fewer than 168 a thread at launch that would be for good.  Only the good answer is kept: a query may fail for
+    // another call's error.
+    static std::atomic<bool> enough{false};
+    cudaError_t e = cudaSuccess;
+    if (!enough.load(std::memory_order_relaxed)) {
         cudaFuncAttributes a;
-        return cudaFuncGetAttributes(&a, kernel) == cudaSuccess && a.numRegs >= kLaunchRegisters;
-    }();
-    if (!enough) { record_cuda_error(cudaErrorInvalidDeviceFunction); return SSD_ERR_CUDA; }
-    cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void *>(kernel), Shape<D>::kBytes);
+        e = cudaFuncGetAttributes(&a, kernel);
+        if (e == cudaSuccess && a.numRegs < kLaunchRegisters) e = cudaErrorInvalidDeviceFunction;
+        if (e == cudaSuccess) enough.store(true, std::memory_order_relaxed);
+    }
+    if (e == cudaSuccess) e = ensure_dynamic_smem(reinterpret_cast<const void *>(kernel), Shape<D>::kBytes);
     if (e == cudaSuccess) e = launch_pdl(kernel, (unsigned)grid, kWarps * 32u, (size_t)Shape<D>::kBytes, stream, p);
     if (e == cudaSuccess)
         e = launch_pdl(tree_attention_join<T, D, kCap>, (unsigned)(grid * kJoinBlocks), (unsigned)kJoinThreads, 0, stream, p, grid);
@@ -939,15 +945,20 @@ bool encode_map(CUtensorMap *map, ssd_dtype dtype, const void *base, int rank, c
     using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
                                 const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-    static const Encode encode = [] {
+    static std::atomic<Encode> known{nullptr};         // kept once it is there: a query may fail for another call's error
+    Encode encode = known.load(std::memory_order_relaxed);
+    if (!encode) {
         void *f = nullptr;
         cudaDriverEntryPointQueryResult found;
         if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found) != cudaSuccess ||
-            found != cudaDriverEntryPointSuccess)
-            f = nullptr;
-        return reinterpret_cast<Encode>(f);
-    }();
-    if (!encode) { cudaGetLastError(); record_cuda_error(cudaErrorNotSupported); return false; }
+            found != cudaDriverEntryPointSuccess || !f) {
+            cudaGetLastError();
+            record_cuda_error(cudaErrorNotSupported);
+            return false;
+        }
+        encode = reinterpret_cast<Encode>(f);
+        known.store(encode, std::memory_order_relaxed);
+    }
     const cuuint32_t ones[5] = {1, 1, 1, 1, 1};
     const CUresult r = encode(map, dtype == SSD_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16,
                               (cuuint32_t)rank, const_cast<void *>(base), dims, strides, box, ones,
