@@ -922,7 +922,7 @@ struct AttnPlan {
     size_t cuts_bytes, bytes;
 };
 // grid: a CTA per multiprocessor, or per tile where there cannot be that many
-AttnPlan attention_plan(int Hq, int Hkv, int D, int64_t M, int max_nodes, int B, int64_t room, int sms) {
+AttnPlan attention_plan(int Hq, int Hkv, int D, int64_t M, int max_nodes, int B, int64_t max_pages, int page, int sms) {
     AttnPlan a;
     const int G = Hq / Hkv;
     if (max_nodes > M) max_nodes = (int)M;
@@ -930,7 +930,8 @@ AttnPlan attention_plan(int Hq, int Hkv, int D, int64_t M, int max_nodes, int B,
     if (a.npt > max_nodes) a.npt = max_nodes > 0 ? max_nodes : 1;      // no more of q is fetched than a tree can have
     a.part_rows = ((max_nodes > a.npt ? 2 : 1) * a.npt * G + 3) / 4 * 4;      // sums begin on 16 bytes
     const int64_t items = (int64_t)B * Hkv * ((max_nodes + 2 * a.npt - 1) / (2 * a.npt));
-    const int64_t tiles = (max_nodes + kTile - 1) / kTile + (room + 7) / 8;      // a tile has 8 slots at least, or a page
+    const int least = page < 8 ? page : 8;                              // of a tile's slots, but for a cache's last
+    const int64_t tiles = (max_nodes + kTile - 1) / kTile + (max_pages * page + least - 1) / least;
     a.grid = items < sms && items * tiles < sms ? (int)(items * tiles) : sms;
     if (a.grid < 1) a.grid = 1;
     a.cuts_bytes = ((size_t)sms * sizeof(Cut) + 255) / 256 * 256;
@@ -986,7 +987,7 @@ bool encode_cache(CUtensorMap *map, const ssd_kv_cache &c, const void *data, int
 size_t tree_attention_workspace_bytes(int Hq, int Hkv, int D, int64_t M, int max_nodes) {
     int sms = device_sm_count();
     if (sms <= 0) sms = 148;                          // without a device: the part that the kernels are made for
-    return attention_plan(Hq, Hkv, D, M, max_nodes, 1, 0, sms).bytes;
+    return attention_plan(Hq, Hkv, D, M, max_nodes, 1, 0, 1, sms).bytes;
 }
 
 int launch_tree_attention(const ssd_heads &q, const ssd_heads &tree_k, const ssd_heads &tree_v, const ssd_kv_cache &cache,
@@ -1001,7 +1002,7 @@ int launch_tree_attention(const ssd_heads &q, const ssd_heads &tree_k, const ssd
     p.G = q.heads / cache.heads;
     const int D = cache.head_dim;
     p.max_pages = cache.pages > 0 ? cache.max_pages : 0;      // without pages every cache is empty
-    const AttnPlan plan = attention_plan(q.heads, cache.heads, D, M, max_nodes, B, (int64_t)p.max_pages * cache.page_size, sms);
+    const AttnPlan plan = attention_plan(q.heads, cache.heads, D, M, max_nodes, B, p.max_pages, cache.page_size, sms);
     p.npt = plan.npt;
     p.part_rows = plan.part_rows;
     p.cuts = static_cast<Cut *>(workspace);

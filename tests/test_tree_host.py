@@ -102,3 +102,15 @@ def test_an_error_of_the_runtime_is_not_remembered(program, call):
 
 def test_a_kernel_of_too_few_registers_is_never_launched(program):
     assert program("registers=160", ONE, ONE) == ["answer 5 98"] * 2
+
+
+@pytest.mark.parametrize("page", [1, 2, 3, 7])
+def test_small_pages_get_as_many_ctas_as_they_have_tiles(program, page):
+    """A page of fewer than 8 slots is a tile of its own: two heads of a node and of 20 pages are 42 tiles."""
+    out = program("%d,20,1,1" % page)
+    assert out[0] == "launch 42 384" and out[-1] == "answer 0 0"
+
+
+def test_small_calls_of_larger_pages_launch_what_they_did(program):
+    for case, grid in (("8,20,1,1", 42), ("16,20,1,1", 82), ("16,100,1,1", 148), ("64,1,3,2", 36), ("100,1,1,1", 28)):
+        assert program(case)[0] == "launch %d 384" % grid, case
