@@ -340,6 +340,11 @@ void *here(const at::Tensor &t) {
     if (t.get_device() != c10::cuda::current_device()) throw Unhandled{};
     return p;
 }
+Scratch scratch_here(PyObject *o) {
+    const Scratch ws = scratch(o, true);
+    here(tensor(o));
+    return ws;
+}
 ssd_dtype kv_type(const at::Tensor &t) {
     if (t.scalar_type() == at::kBFloat16) return SSD_BF16;
     if (t.scalar_type() == at::kHalf) return SSD_F16;
@@ -440,7 +445,7 @@ PyObject *tree_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
             if (x->dtype != q.dtype || x->rows != q.rows || x->D != q.D) throw Unhandled{};
         if (c.dtype != q.dtype || c.head_dim != q.D || o.h.heads != q.h.heads) throw Unhandled{};
         float *lse = per_head(entry(a[12], K_lse), q.rows, q.h.heads, true);
-        const Scratch ws = scratch(entry(a[12], K_workspace), true);
+        const Scratch ws = scratch_here(entry(a[12], K_workspace));
         auto *us = flat<uint32_t>(entry(a[12], K_utt_status), at::kInt, B, false);
         void *st = stream();
         return [=] {
@@ -469,7 +474,7 @@ PyObject *verify_tree(PyObject *, PyObject *const *a, Py_ssize_t n) {
         auto *len = flat<int32_t>(entry(o, K_path_len), at::kInt, B, false);
         auto *on = flat<uint8_t>(entry(o, K_on_path), at::kByte, x.n, false);
         auto *us = flat<uint32_t>(entry(o, K_utt_status), at::kInt, B, false);
-        const Scratch ws = scratch(entry(o, K_workspace), true);
+        const Scratch ws = scratch_here(entry(o, K_workspace));
         void *st = stream();
         return [=] {
             return ssd_verify_tree(x.p, x.dtype, (int32_t)x.V, x.ld, off, ids, parent, B, x.n, tau, skip, logp, lse, path, len, on, us,
