@@ -349,3 +349,17 @@ def test_weights_at_caps_whose_ratio_to_the_scale_is_no_normal_number(cuda_devic
     got, status = run_weights(c, cuda_device, lse, cap=cap)
     want = weights(c, lse, None, cap)
     assert ((got.cpu().double() - want).abs() <= 1e-5 * want + 1e-12).all() and not status.any()
+
+
+@pytest.mark.parametrize("budget,sink,recent", [(20_000, 4, 512), (32_768, 0, 0), (100, 0, 100)])
+def test_evict_of_caches_longer_than_shared_memory_holds(cuda_device, budget, sink, recent):
+    """Weights of up to 32,768 slots are held in shared memory, longer ones are read where they lie; both in one call."""
+    rng = np.random.default_rng(7)
+    c = Case(45, [1] * 5, [100_000, 9, 32_768, 32_769, 40_001], Hq=1, Hkv=1, page=64)
+    W = 100_000
+    w = np.exp(2 * rng.standard_normal((c.B, W))).astype(np.float32)
+    check_evict(c, cuda_device, w, budget, sink, recent)
+    check_evict(c, cuda_device, rng.integers(0, 4, (c.B, W)).astype(np.float32), budget, sink, recent, inplace=True)     # ties
+    w = rng.standard_normal((c.B, W)).astype(np.float32)
+    w[:, ::3], w[:, 1::7], w[:, 2::11] = np.nan, -np.inf, -0.0
+    check_evict(c, cuda_device, w, budget, sink, recent)
