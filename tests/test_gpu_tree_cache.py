@@ -363,3 +363,41 @@ def test_evict_of_caches_longer_than_shared_memory_holds(cuda_device, budget, si
     w = rng.standard_normal((c.B, W)).astype(np.float32)
     w[:, ::3], w[:, 1::7], w[:, 2::11] = np.nan, -np.inf, -0.0
     check_evict(c, cuda_device, w, budget, sink, recent)
+
+
+def test_offsets_that_pass_32_bits(cuda_device):
+    """A cache of more than 2^31 values whose pages in use are its last ones, and rows of nodes 2^26 values apart: through
+    every call on a cache, against the same calls on compact arrays."""
+    c = Case(46, [40, 3], [150, 90], Hq=8, Hkv=2, D=128, room=40, chain=True)
+    dev, d = cuda_device, c.on(cuda_device)
+    pages = 2**31 // c.k[0].numel() + 100
+    shift = pages - c.k.shape[0]
+    big = {}
+    for name in ("k", "v"):
+        big[name] = torch.empty((pages, *c.k.shape[1:]), dtype=c.dtype, device=dev)
+        big[name][shift:] = d[name]
+    assert big["k"].numel() > 2**31
+    wide = torch.empty((c.M, 2**26), dtype=c.dtype, device=dev)
+    at = 0
+    for name, heads in (("q", 8), ("tk", 2), ("tv", 2), ("out", 8)):
+        big[name] = wide[:, at:at + heads * 128].view(c.M, heads, 128)
+        at += heads * 128
+        if name != "out":
+            big[name].copy_(d[name])
+    used = (torch.arange(c.table.shape[1])[None] < torch.from_numpy(-(-(c.lens + 40) // c.page))[:, None]).to(dev)
+    big["table"] = torch.where(used, d["table"] + shift, 2**30)
+    path_len = torch.tensor([33, 2], dtype=torch.int32, device=dev)
+    results = []
+    for x in (d, {**d, **big}):
+        att = ssd.alloc_tree_attention_outputs(c.M, 2, 8, 128, c.dtype, dev, 2, c.max_nodes)
+        att["out"] = x.get("out", att["out"])
+        ssd.ssd_tree_attention(x["q"], x["tk"], x["tv"], x["k"], x["v"], x["table"], x["lens"], x["off"], c.max_nodes, None, out=att)
+        weight = torch.zeros(2, 200, device=dev)
+        ssd.ssd_cache_weights(x["q"], att["lse"], x["k"], x["table"], x["lens"], x["off"], c.max_nodes, weight)
+        app = ssd.ssd_cache_append(x["tk"], x["tv"], x["off"], None, path_len, x["k"], x["v"], x["table"], x["lens"], weight)
+        evi = ssd.ssd_cache_evict(x["k"], x["v"], x["table"], app["new_len"], weight, 64, 2, 8)
+        results.append(cpu(dict(out=att["out"], lse=att["lse"], weight=weight, k=x["k"][-c.k.shape[0]:], v=x["v"][-c.k.shape[0]:],
+                                **{"evict " + k: v for k, v in evi.items()})))
+    for k in results[0]:
+        assert torch.equal(results[0][k], results[1][k]), k
+    assert (results[0]["evict new_len"] == 64).all() and not results[0]["evict utt_status"].any()
