@@ -415,7 +415,9 @@ int32_t ssd_verify_combine(const float *stats_all, int32_t R, int64_t V_total,
  * Keys, values, queries and attention outputs are SSD_BF16 or SSD_F16, heads are 64 or 128 values
  * long and contiguous; every base address and every stride of an axis with more than one entry is a
  * multiple of 16 bytes (else SSD_ERR_ALIGN).  Strides count elements.  A cache has at most 2^31 - 1
- * slots, an utterance at most 2^31 - 257.
+ * slots, an utterance at most 2^31 - 257.  A page may have any number of slots, but the calls that read
+ * keys do best with 8, 16, 24, ... 64 or with 65 and more: another page is fetched, and paid for, as the
+ * 128 slots of a whole tile (pages of one slot: 50 times the time).
  */
 typedef struct ssd_heads {     /* an array [M, heads, head_dim] */
     void *data;
@@ -436,6 +438,7 @@ typedef struct ssd_kv_cache {  /* k and v: [pages, page_size, heads, head_dim], 
 /*
  * Attention of every node to its utterance's cache and to its own line of descent.
  *   s_ij   = scale q_i . k_j,  or  cap tanh(scale q_i . k_j / cap)  where cap > 0
+ *            (a cap of more than 8e37 times the scale is above every score, and taken as none)
  *   out_i  = sum_j softmax_j(s_ij) v_j     over the cached slots and the nodes of i's line
  *   lse[i, head] = log sum_j exp(s_ij)                                            (nullable)
  * q [M, Hq, D], tree_k, tree_v [M, Hkv, D], out [M, Hq, D] (same type); Hq a multiple of Hkv, at most

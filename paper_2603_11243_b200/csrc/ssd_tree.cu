@@ -20,8 +20,9 @@
 // closing kernel joins.
 //
 // Measured (32 query and 8 kv heads of 128, bf16, pages of 16): trees of 5 to 32 nodes on 64 caches of 500 to
-// 3,000 slots 119 us, 475 MB at 4.0 TB/s; chains of 50 to 200 nodes on 128 caches of 250 to 1,500 slots 490 us, 256 GFLOP at
-// 522 TFLOP/s.  A key tile takes a CTA 2,400 clocks either way: at few rows that is what HBM gives a
+// 3,000 slots 119 us, 475 MB at 4.0 TB/s; chains of 50 to 200 nodes on 128 caches of 250 to 1,500 slots 488 us, 256 GFLOP at
+// 523 TFLOP/s.  (Comments below give times before and after a step on one box each; boxes differ by up to 15 % where the
+// power limit is reached.)  A key tile takes a CTA 2,400 clocks either way: at few rows that is what HBM gives a
 // multiprocessor, at many it is the cycle scores -> softmax -> product of a stream (4,500 clocks) over two streams, of
 // which the products are 1,220 and the softmax 2,250.
 #include <math.h>
@@ -734,7 +735,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tree_attention(const __grid_co
         pos0 += 2 * tiles;
         // ---- what came of it ------------------------------------------------------------------------
         // A pair's streams have nothing to do with one another: each ends when it does (chains 484 -> 461 us against a
-        // meeting).  Those of one tile meet.
+        // meeting, 494 -> 480 on another box).  Those of one tile meet.
         if (!pair) ml[s * kTile + row] = make_float2(m, l);
         const bool any[2] = {true, pair || tiles > 1};                 // whether a stream had tiles
         for (int i = 0; i < 2; ++i)
