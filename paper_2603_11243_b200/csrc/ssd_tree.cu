@@ -908,6 +908,7 @@ int launch(const AttnParams &p, int grid, cudaStream_t stream) {
         e = cudaFuncGetAttributes(&a, kernel);
         if (e == cudaSuccess && a.numRegs < kLaunchRegisters) e = cudaErrorInvalidDeviceFunction;
         if (e == cudaSuccess) enough.store(true, std::memory_order_relaxed);
+        else cudaGetLastError();                       // or the next call finds it behind its own launch
     }
     if (e == cudaSuccess) e = ensure_dynamic_smem(reinterpret_cast<const void *>(kernel), Shape<D>::kBytes);
     if (e == cudaSuccess) e = launch_pdl(kernel, (unsigned)grid, kWarps * 32u, (size_t)Shape<D>::kBytes, stream, p);

@@ -18,7 +18,11 @@ PROGRAM = r"""
 
 static const char *failing = "";          // the runtime call that fails
 static int registers = 168;
-static bool fails(const char *name) { return !strcmp(failing, name); }
+static cudaError_t last = cudaSuccess;    // what cudaGetLastError has to tell, once
+static cudaError_t result(const char *name, cudaError_t error) {
+    if (strcmp(failing, name)) return cudaSuccess;
+    return last = error;
+}
 
 static CUresult encode(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
                        const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill) {
@@ -31,12 +35,12 @@ cudaError_t cudaDeviceGetAttribute(int *v, cudaDeviceAttr, int) { *v = 148; retu
 cudaError_t cudaFuncGetAttributes(cudaFuncAttributes *a, const void *) {
     memset(a, 0, sizeof *a);
     a->numRegs = registers;
-    return fails("cudaFuncGetAttributes") ? cudaErrorLaunchFailure : cudaSuccess;
+    return result("cudaFuncGetAttributes", cudaErrorLaunchFailure);
 }
 cudaError_t cudaFuncSetAttribute(const void *, cudaFuncAttribute, int) { return cudaSuccess; }
-cudaError_t cudaGetLastError(void) { return cudaSuccess; }
+cudaError_t cudaGetLastError(void) { const cudaError_t e = last; last = cudaSuccess; return e; }
 cudaError_t cudaGetDriverEntryPointByVersion(const char *, void **f, unsigned, unsigned long long, cudaDriverEntryPointQueryResult *r) {
-    const bool bad = fails("cudaGetDriverEntryPointByVersion");
+    const bool bad = result("cudaGetDriverEntryPointByVersion", cudaErrorInitializationError) != cudaSuccess;
     *f = bad ? nullptr : (void *)encode;
     if (r) *r = bad ? cudaDriverEntryPointSymbolNotFound : cudaDriverEntryPointSuccess;
     return bad ? cudaErrorInitializationError : cudaSuccess;
